@@ -1,0 +1,159 @@
+"""Binding of the AdamW step (``include/adamw.h``): argument marshalling only.
+
+``adamw_state`` makes the states, ``adamw_step`` updates parameters and states in place on the current stream.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+from typing import NamedTuple, Optional, Sequence, Union
+
+import numpy as np
+import torch
+
+from .binding import JsError, JS_ERR_ARG, load_library, _stream_ptr
+
+ADAMW_OK, ADAMW_ERR_INVALID, ADAMW_ERR_CUDA = 0, -1, -2
+ADAMW_BLOCK = 256
+
+
+class AdamWState(NamedTuple):
+    """m and v of all tensors: tensor i's values start at the sum of the sizes before it, each rounded up to a multiple of 256.
+    32 bits: float32, scales None.  8 bits: float8_e4m3fn with a float32 scale for every 256 places; v holds its square root."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+class _Options(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_longlong), ("step_dev", C.c_void_p), ("lr_dev", C.c_void_p), ("grad_scale", C.c_void_p), ("skip", C.c_void_p),
+                ("seed", C.c_longlong)]
+
+
+_ready = False
+
+
+def _lib():
+    global _ready
+    lib = load_library()
+    if not _ready:
+        vp = C.c_void_p
+        lib.adamw_step.argtypes = [vp, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, C.POINTER(_Options), vp]
+        lib.adamw_last_error.restype = C.c_char_p
+        _ready = True
+    return lib
+
+
+def _bad(what: str):
+    raise JsError(JS_ERR_ARG, what)
+
+
+def _places(sizes):
+    return sum((n + ADAMW_BLOCK - 1) // ADAMW_BLOCK * ADAMW_BLOCK for n in sizes)
+
+
+def adamw_state(params: Sequence[torch.Tensor], bits: int = 32) -> AdamWState:
+    """States of zeros for these parameters, on their device."""
+    if bits not in (32, 8):
+        _bad("bits: 32 or 8")
+    if not params:
+        _bad("params: no tensors")
+    n, device = _places([p.numel() for p in params]), params[0].device
+    if bits == 32:
+        return AdamWState(torch.zeros(n, dtype=torch.float32, device=device), torch.zeros(n, dtype=torch.float32, device=device))
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    ms, vs = (torch.full((n // ADAMW_BLOCK,), 2.0 ** -120, dtype=torch.float32, device=device) for _ in range(2))
+    return AdamWState(m, v, ms, vs)
+
+
+def _one(t, dtype, device, what):
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.numel() == 1 and t.device == device):
+        _bad(f"{what}: expected one {dtype} on the parameters' device")
+    return t.data_ptr()
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], state: AdamWState, step: Union[int, torch.Tensor],
+               lr: Union[float, torch.Tensor], betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+               copies: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None,
+               skip: Optional[torch.Tensor] = None, seed: Optional[int] = None, stream=None) -> None:
+    """One step on all tensors, in place.
+
+    params      float32, contiguous, no two the same; grads of the same sizes, all float32 or all bfloat16, contiguous
+    state       from ``adamw_state`` (or a tuple laid out like it)
+    step        number of the step, 1 or more; or an int64 tensor on the device, which a captured call reads anew at every replay
+    lr          learning rate; or a float32 tensor on the device
+    copies      bfloat16 tensors that take the new parameters rounded, for the next forward pass
+    grad_scale  one float32 on the device: factor of all gradients
+    skip        one int32 on the device: not zero leaves everything as it is (a step whose gradients overflowed)
+    seed        of the random roundings of 8-bit states (the step's number if None)
+    """
+    n = len(params)
+    m, v, m_scale, v_scale = state
+    if len(grads) != n or (copies is not None and len(copies) != n):
+        _bad("params, grads and copies: as many tensors of each")
+    if n == 0:
+        return
+    device, f32 = params[0].device, torch.float32
+    if device.type != "cuda":
+        _bad("params: expected CUDA tensors")
+    gtype = grads[0].dtype
+    if gtype not in (f32, torch.bfloat16):
+        _bad("grads: expected float32 or bfloat16")
+    sizes = [p.numel() for p in params]
+    if not all([p.dtype is f32 and p.device == device and p.is_contiguous() for p in params]):
+        _bad("params: expected contiguous float32 tensors on one device")
+    if not all([g.dtype is gtype and g.device == device and g.is_contiguous() and g.numel() == k for g, k in zip(grads, sizes)]):
+        _bad("grads: expected contiguous tensors of one type, of the parameters' sizes and on their device")
+    if copies is not None and not all([t.dtype is torch.bfloat16 and t.device == device and t.is_contiguous() and t.numel() == k
+                                       for t, k in zip(copies, sizes)]):
+        _bad("copies: expected contiguous bfloat16 tensors of the parameters' sizes and on their device")
+    bits = 32 if m.dtype is f32 else 8
+    stype, places = (f32 if bits == 32 else torch.float8_e4m3fn), _places(sizes)
+    for t, what in ((m, "m"), (v, "v")):
+        if not (t.dtype is stype and t.device == device and t.is_contiguous() and t.numel() == places):
+            _bad(f"state.{what}: expected {places} contiguous values of {stype} on the parameters' device")
+    for t, what in ((m_scale, "m_scale"), (v_scale, "v_scale")):
+        if bits == 8 and not (t is not None and t.dtype is f32 and t.device == device and t.is_contiguous() and t.numel() == places // ADAMW_BLOCK):
+            _bad(f"state.{what}: expected {places // ADAMW_BLOCK} contiguous float32 on the parameters' device")
+    table = np.zeros((n, 4), dtype=np.int64)
+    ptrs = [p.data_ptr() for p in params]
+    live = [a for a, k in zip(ptrs, sizes) if k]
+    if len(set(live)) != len(live):
+        _bad("params: the same tensor twice")
+    table[:, 0] = ptrs
+    table[:, 1] = [g.data_ptr() for g in grads]
+    if copies is not None:
+        table[:, 2] = [t.data_ptr() for t in copies]
+    table[:, 3] = sizes
+    o = _Options(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=-1 if seed is None else int(seed) & 0xFFFFFFFF)
+    if isinstance(step, torch.Tensor):
+        o.step_dev = _one(step, torch.int64, device, "step")
+    else:
+        o.step = int(step)
+    if isinstance(lr, torch.Tensor):
+        o.lr_dev = _one(lr, f32, device, "lr")
+    else:
+        o.lr = float(lr)
+    o.grad_scale = _one(grad_scale, f32, device, "grad_scale")
+    o.skip = _one(skip, torch.int32, device, "skip")
+    with _on(device):
+        rc = _lib().adamw_step(table.ctypes.data, n, 0 if gtype is f32 else 1, bits, m.data_ptr(), v.data_ptr(),
+                               m_scale.data_ptr() if bits == 8 else None, v_scale.data_ptr() if bits == 8 else None, C.byref(o), _stream_ptr(stream))
+    if rc != ADAMW_OK:
+        raise JsError(rc, "adamw_step: " + (_lib().adamw_last_error().decode() if rc == ADAMW_ERR_CUDA else "argument outside the documented limits"))
+
+
+def _on(device):
+    """The tensors' device as the current one, for the call."""
+    if device.index == torch._C._cuda_getDevice():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _stream(stream):
+    """New tensors belong to the stream that the call runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
