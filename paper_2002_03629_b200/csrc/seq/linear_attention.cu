@@ -4,15 +4,14 @@
 #include <cmath>
 #include <cstdio>
 
-#include "la_common.cuh"
+#include "la_tc.h"
 
 namespace {
 
 thread_local char g_err[256] = "";
 
-int launched()
+int status(cudaError_t e)
 {
-    const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return LA_OK;
     snprintf(g_err, sizeof g_err, "%s", cudaGetErrorString(e));
     return LA_ERR_CUDA;
@@ -192,26 +191,32 @@ bool tensor_ok(const la_shape *s, const la_tensor *t, long long rows)
     return t->data != nullptr && (reinterpret_cast<uintptr_t>(t->data) & (s->type == LA_F32 ? 3u : 1u)) == 0;
 }
 
-int run(const la_shape *s, const LaJobs &jobs, int count, cudaStream_t stream)
+int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const *tensors, int n_in, int n_all, const int (*which)[3], void *workspace,
+        cudaStream_t stream)
 {
     const LaSeqs seqs{s->cu_seqlens != nullptr ? s->N : s->B, s->H, s->T, s->cu_seqlens, s->log_decay};
     if (seqs.n == 0) return LA_OK;
+    bool aligned = (reinterpret_cast<uintptr_t>(workspace) & 15u) == 0;
+    for (int j = 0; j < count; ++j)
+        aligned = aligned && ((reinterpret_cast<uintptr_t>(jobs.job[j].s0) | reinterpret_cast<uintptr_t>(jobs.job[j].s1)) & 15u) == 0;
+    if (aligned && la_tc_takes(s, tensors, n_all)) return status(la_tc_run(s, jobs, count, tensors, n_in, which, workspace, stream));
     int dv = 0;
     for (int j = 0; j < count; ++j) dv = std::max(dv, jobs.job[j].Dv);
     auto kernel = s->type == LA_F32 ? la_any_kernel<float> : la_any_kernel<__nv_bfloat16>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G_SMEM) != cudaSuccess) return launched();
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G_SMEM) != cudaSuccess) return status(cudaGetLastError());
     kernel<<<dim3((unsigned)(seqs.n * s->H), (dv + VS - 1) / VS, count), GTH, G_SMEM, stream>>>(jobs, seqs);
-    return launched();
+    return status(cudaGetLastError());
 }
 
 }  // namespace
 
 extern "C" {
 
+// (What the tensor-core path needs, taken or not: whether the tensors may go that way is seen with them.)
 size_t la_workspace(const la_shape *s, int backward)
 {
-    (void)backward;
-    return shape_ok(s) ? 16 : 0;
+    if (!shape_ok(s)) return 0;
+    return std::max<size_t>(16, s->type == LA_BF16 && s->Dk % 16 == 0 && s->Dv % 16 == 0 ? la_tc_plan(s, backward ? 3 : 1).bytes : 0);
 }
 
 int la_forward(const la_shape *s, const la_tensor *q, const la_tensor *k, const la_tensor *v, const float *state0, const la_tensor *o,
@@ -221,10 +226,13 @@ int la_forward(const la_shape *s, const la_tensor *q, const la_tensor *k, const 
     const long long rows = s->B * s->T;
     for (const la_tensor *t : {q, k, v, o})
         if (!tensor_ok(s, t, rows)) return LA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(state0) | reinterpret_cast<uintptr_t>(state)) & 3u) return LA_ERR_INVALID;
     if (workspace_bytes < la_workspace(s, 0) || workspace == nullptr) return LA_ERR_INVALID;
     LaJobs jobs{};
     jobs.job[0] = LaJob{*q, *k, *v, *o, state0, state, s->Dk, s->Dv, 0, 0, 1.0f, s->scale};
-    return run(s, jobs, 1, (cudaStream_t)stream);
+    const la_tensor *all[] = {q, k, v, o};
+    static const int which[1][3] = {{0, 1, 2}};
+    return run(s, jobs, 1, all, 3, 4, which, workspace, (cudaStream_t)stream);
 }
 
 int la_backward(const la_shape *s, const la_tensor *q, const la_tensor *k, const la_tensor *v, const float *state0, const la_tensor *d_o,
@@ -235,12 +243,15 @@ int la_backward(const la_shape *s, const la_tensor *q, const la_tensor *k, const
     const long long rows = s->B * s->T;
     for (const la_tensor *t : {q, k, v, d_o, dq, dk, dv})
         if (!tensor_ok(s, t, rows)) return LA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(state0) | reinterpret_cast<uintptr_t>(dstate) | reinterpret_cast<uintptr_t>(dstate0)) & 3u) return LA_ERR_INVALID;
     if (workspace_bytes < la_workspace(s, 1) || workspace == nullptr) return LA_ERR_INVALID;
     LaJobs jobs{};
     jobs.job[0] = LaJob{*k, *q, *d_o, *dv, dstate, dstate0, s->Dk, s->Dv, 1, 0, s->scale, 1.0f};
     jobs.job[1] = LaJob{*v, *d_o, *q, *dk, dstate, nullptr, s->Dv, s->Dk, 1, 1, s->scale, 1.0f};
     jobs.job[2] = LaJob{*d_o, *v, *k, *dq, state0, nullptr, s->Dv, s->Dk, 0, 1, 1.0f, s->scale};
-    return run(s, jobs, 3, (cudaStream_t)stream);
+    const la_tensor *all[] = {q, k, v, d_o, dq, dk, dv};
+    static const int which[3][3] = {{1, 0, 3}, {2, 3, 0}, {3, 2, 1}};
+    return run(s, jobs, 3, all, 4, 7, which, workspace, (cudaStream_t)stream);
 }
 
 int la_step(const la_shape *s, const la_tensor *q, const la_tensor *k, const la_tensor *v, float *state, const la_tensor *o, void *stream)
@@ -256,7 +267,7 @@ int la_step(const la_shape *s, const la_tensor *q, const la_tensor *k, const la_
     auto kernel = s->type == LA_F32 ? (vec ? la_step_kernel<float, true> : la_step_kernel<float, false>)
                                     : (vec ? la_step_kernel<__nv_bfloat16, true> : la_step_kernel<__nv_bfloat16, false>);
     kernel<<<(unsigned)(s->B * s->H), STH, 0, (cudaStream_t)stream>>>(*q, *k, *v, state, *o, s->log_decay, s->scale, s->H, s->Dk, s->Dv, width);
-    return launched();
+    return status(cudaGetLastError());
 }
 
 const char *la_last_error(void) { return g_err; }
