@@ -199,7 +199,7 @@ int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const
     bool aligned = (reinterpret_cast<uintptr_t>(workspace) & 15u) == 0;
     for (int j = 0; j < count; ++j)
         aligned = aligned && ((reinterpret_cast<uintptr_t>(jobs.job[j].s0) | reinterpret_cast<uintptr_t>(jobs.job[j].s1)) & 15u) == 0;
-    if (aligned && la_tc_takes(s, tensors, n_all)) return status(la_tc_run(s, jobs, count, tensors, n_in, which, workspace, stream));
+    if (aligned && la_tc_takes(s, count, tensors, n_all)) return status(la_tc_run(s, jobs, count, tensors, n_in, which, workspace, stream));
     int dv = 0;
     for (int j = 0; j < count; ++j) dv = std::max(dv, jobs.job[j].Dv);
     auto kernel = s->type == LA_F32 ? la_any_kernel<float> : la_any_kernel<__nv_bfloat16>;

@@ -5,15 +5,17 @@
 // in the chunk, weights w_j = lambda^(rows-1-j) and the state S before it:
 //     scores = Q K^T;   P = scores * lambda^(i-j), j <= i;   U = (w K)^T V;   O = lambda^(i+1) (Q S) + P V;   S = lambda^rows S + U
 // Backwards in time the tiles lie in memory order all the same and the position of row r is rows-1-r.
-// Roles, five groups of four warps:
-//   P    scores from tensor memory, masked and decayed, as bf16 back over them: the left operand of P V
-//   K    K from shared memory, weighted in fp32 and cut into two or three bf16 pieces, into tensor memory (transposed on the way: a
-//        thread is a row of K^T): the left operand of U.  One piece would leave the fp32 state off by 2^-9; two 1e-6, where nobody asks for
-//        the state; three 5e-7.
-//   S    the state in registers, fp32, one row of Dv values a thread; rounded to bf16 into shared memory for Q S
-//   O    Q S scaled by lambda^(i+1) in tensor memory, later the sum out to memory
-//   C    a warp that loads tiles (TMA, a ring of stages that runs on across chunks and units) and one that issues the MMAs
-// P, the scores of its other half and K's third piece share 128 columns of tensor memory, U, O and K's other pieces take 128 each: all 512.
+// Roles:
+//   P, O  four warps: scores from tensor memory, masked and decayed, as bf16 back over them (the left operand of P V); then the chunk before's
+//         outputs to memory.  Under strong decay Q S is scaled by lambda^(i+1) in tensor memory before P V is added.
+//   K, S  eight warps: K from shared memory, transposed on the way, weighted and cut into two or three bf16 pieces (the left operand of
+//         U; one piece would leave the fp32 state off by 2e-3, three leave 5e-7; two, off by 3e-6, do where nobody asks for the state): two into
+//         tensor memory, the third back to where K was.  The state, fp32, in registers, a row of Dv / 2 values a thread; rounded to bf16 into shared
+//         memory for Q S.
+//   a warp that finds units and loads tiles (TMA, a ring of stages that runs on across chunks and units), one that issues the MMAs
+// Tensor memory is full: scores and P over them, U, O and K's pieces take 128 columns each.
+// The roles' loops are kept short and free of what can be done once: unrolled further, or with the search for units in each of them, their code
+// fell out of the instruction cache.  setmaxnreg for one role with a whole row of the state a thread was slower (20 warps, spills in others).
 #include <algorithm>
 #include <cstdio>
 
@@ -24,8 +26,8 @@
 namespace {
 
 constexpr int C = 128;                       // steps of a chunk
-constexpr int GROUPS = 5, TH = GROUPS * 128;
-constexpr uint32_t COL_SC = 0, COL_LOW = 64, COL_U = 128, COL_O = 256, COL_K = 384;
+constexpr int TH = 448;                      // 4 + 8 + 2 warps: four to a scheduler at most, so that a thread may have 128 registers
+constexpr uint32_t COL_SC = 0, COL_U = 128, COL_O = 256, COL_K = 384;      // scores and P; own sum; output; K's upper pieces
 
 struct Params {
     CUtensorMap map[4];
@@ -33,33 +35,33 @@ struct Params {
     int which[3][3];                         // a job's q, k, v: number of the tensor map
     int flat[4];                             // tensors whose batch (1) or head (2) stride is 0: coordinate 0
     LaSeqs seqs;
-    int jobs, slots;                         // slots: segments of all sequences
-    long long seg;                           // steps of a segment, a multiple of C
+    int jobs, slots, per;                    // slots: segments of all sequences; per: of one, where all are alike
+    int seg;                                 // steps of a segment, a multiple of C
+    int units;
     float *carry;                            // [job][slot][head][Dk][Dv]
-    long long units;
 };
 
 struct Unit {
     int job, seq, h, n, c0, c1;              // steps of the sequence, chunks [c0, c1) of it
+    int slot;
     bool last;
-    long long start, slot;
+    long long start;
 };
 
 // Unit u, or false: none.  With cu_seqlens, sequence s owns the slots from cu[s] / seg + s on, at least as many as it has segments.
-__device__ __forceinline__ bool get_unit(const Params &p, long long u, Unit &x)
+__device__ __forceinline__ bool get_unit(const Params &p, int u, Unit &x)
 {
-    x.job = (int)(u % p.jobs);
+    x.job = u % p.jobs;
     u /= p.jobs;
-    x.h = (int)(u % p.seqs.H);
+    x.h = u % p.seqs.H;
     x.slot = u / p.seqs.H;
-    long long s;
+    int s;
     if (p.seqs.cu == nullptr) {
-        const long long per = p.slots / p.seqs.n;
-        x.seq = (int)(x.slot / per);
-        s = x.slot % per;
+        x.seq = x.slot / p.per;
+        s = x.slot % p.per;
     } else {
         int lo = 0, hi = p.seqs.n;
-        auto first = [&](int q) { return min(max((long long)__ldg(p.seqs.cu + q), 0ll), p.seqs.T) / p.seg + q; };
+        auto first = [&](int q) { return min(max(__ldg(p.seqs.cu + q), 0), (int)p.seqs.T) / p.seg + q; };
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (first(mid) <= x.slot) lo = mid;
@@ -70,7 +72,7 @@ __device__ __forceinline__ bool get_unit(const Params &p, long long u, Unit &x)
         if (s < 0) return false;
     }
     x.n = la_sequence(p.seqs, x.seq, x.start);
-    const long long at = s * p.seg;
+    const long long at = (long long)s * p.seg;
     if (s > 0 && at >= x.n) return false;
     const long long end = min(at + p.seg, (long long)x.n);
     x.c0 = (int)(at / C);
@@ -79,27 +81,51 @@ __device__ __forceinline__ bool get_unit(const Params &p, long long u, Unit &x)
     return true;
 }
 
+// What the roles need to know of a chunk.  The loading warp works it out and hands it on through a ring, so that the code that finds
+// units (divisions, searches) is not in every role's loop.
+enum : int { FIRST = 1, LAST = 2, STATE = 4, LATE = 8, WEAK = 16, THREE = 32, BACK = 64, NONE = 128, END = 256 };
+struct alignas(16) Chunk {
+    int flags, rows, job;                    // FIRST, LAST of its unit; STATE: there is one before it; NONE: the unit has no steps
+    float ld, sum_scale, last;               // last: factor of the state that is handed out
+    __nv_bfloat16 *out;                      // first row
+    const float *from;                       // the unit's first state (NULL: zeros) and where its last one goes (NULL: nowhere)
+    float *to;
+    int turned;
+};
+constexpr int RING = 4, ROLE_WARPS = 13;
+
 struct Shared {
-    uint64_t full[4], empty[4];
-    uint64_t sc_full, p_ready, k_ready, low_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
+    uint64_t full[4], empty[4], told[RING], heard[RING];
+    uint64_t sc_full, p_ready, k_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
+    Chunk chunk[RING];
     uint32_t tmem;
     int dead;
-    alignas(16) float near[4][32], wk[4][C];     // a warp's own: powers within a block of 32 columns of P, weights of K
+    // weights of the scores' columns; of K's rows, in fp32 and as two bf16 pieces, rows 2 i and 2 i + 1 in word i.  (A table is written by each
+    // warp of its group, the same values; no warp is then still at the chunk before, whose products a barrier has reported.)
+    alignas(16) float wp[C], wk[C];
+    uint32_t wk1[C / 2], wk2[C / 2];
 };
 
-__device__ __forceinline__ bool la_wait(Shared &sh, uint64_t *bar, uint32_t parity)
+__device__ __forceinline__ bool la_wait(int &dead, uint64_t *bar, uint32_t parity)
 {
     if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = global_ns();
     for (unsigned i = 1;; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 63u) == 0u && (*(volatile int *)&sh.dead || global_ns() - t0 > MBAR_WAIT_NS)) break;
+        if ((i & 63u) == 0u && (*(volatile int *)&dead || global_ns() - t0 > MBAR_WAIT_NS)) break;
     }
-    *(volatile int *)&sh.dead = 1;
+    *(volatile int *)&dead = 1;
     return false;
 }
 // the same by a whole warp, which goes on or ends together
-__device__ __forceinline__ bool warp_wait(Shared &sh, uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, la_wait(sh, bar, parity)); }
+template <typename Sh>
+__device__ __forceinline__ bool warp_wait(Sh &sh, uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, la_wait(sh.dead, bar, parity)); }
+
+// Weak decay: O = lambda^(i+1) (Q S + P' V) with P' = scores * lambda^(-j-1), one weight a column, all powers taken MID steps lower (S times lambda^MID);
+// the sum stays in tensor memory until it is complete.  With lambda^-64 beyond e^44 the products could leave fp32: then P has lambda^(i-j), and
+// Q S is scaled in tensor memory before P V is added.
+constexpr int MID = 64;
+__device__ __forceinline__ float power_of(float log_decay, int n) { return expf((float)n * log_decay); }
 
 // D[tmem] (+)= A[tmem] * B[smem], 128 x N x 16
 __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate)
@@ -113,11 +139,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
                    "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -130,12 +151,56 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
 {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ float lds_bf16(uint32_t at)
+// Four 8 x 8 blocks of 16-bit values, transposed: lane i gets values 2 (i % 4) and the next of row i / 4 of each block's transpose; lane i's address is
+// that of row i % 8 of block i / 8.
+__device__ __forceinline__ void ldsm4_t(uint32_t at, uint32_t (&r)[4])
 {
-    uint16_t r;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(at));
-    return __uint_as_float((uint32_t)r << 16);
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
+// the same values back to where they came from
+__device__ __forceinline__ void stsm4_t(uint32_t at, const uint32_t (&r)[4])
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+// Eight columns of sixteen lanes over a warp: lane i holds column i % 4 of lanes i / 4 (r[0]) and i / 4 + 8 (r[1]), and the same of the next four columns
+__device__ __forceinline__ void tmem_st_16x8(uint32_t taddr, const uint32_t (&r)[4])
+{
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+// two fp32 values in a register pair, and operations on both
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float lo, float hi)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float lo(f2 x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float hi(f2 x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// two bf16 values as fp32, and back
+__device__ __forceinline__ f2 wide(uint32_t x) { return pair(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+__device__ __forceinline__ f2 wide_negative(uint32_t x) { x ^= 0x80008000u; return wide(x); }
+__device__ __forceinline__ uint32_t narrow(f2 x) { return pack_bf16x2(lo(x), hi(x)); }
+__device__ __forceinline__ __nv_bfloat162 as_bf2(uint32_t x) { return *reinterpret_cast<__nv_bfloat162 *>(&x); }
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t *>(&x); }
 // a warp's arrival, its tensor-memory accesses before it
 __device__ __forceinline__ void tmem_arrive(uint64_t *bar)
 {
@@ -146,12 +211,118 @@ __device__ __forceinline__ void tmem_arrive(uint64_t *bar)
 // 128-byte swizzled tile: rows of 64 bf16; operand with N together ("MN-major"), panels of 64 columns `panel` bytes apart
 __device__ __forceinline__ uint64_t desc_mn(uint32_t at, uint32_t panel) { return smem_desc_sw128(at) + ((uint64_t)((panel >> 4) - 1) << 16); }
 
+// Sixteen words of P from 32 scores: times the columns' weights; columns not in `keep` are zero, whatever they hold
+__device__ __forceinline__ void p_pack(uint32_t (&s)[32], uint32_t (&w)[16], const float *weights, uint32_t keep)
+{
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        ulonglong2 r = *reinterpret_cast<const ulonglong2 *>(weights + e);
+        r.x = mul2(r.x, pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+        r.y = mul2(r.y, pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])));
+        w[e / 2] = narrow(r.x);
+        w[e / 2 + 1] = narrow(r.y);
+    }
+    if (keep != 0xffffffffu)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] &= (keep >> (2 * e) & 1u ? 0xffffu : 0u) | (keep >> (2 * e + 1) & 1u ? 0xffff0000u : 0u);
+}
+
+// Weights of K's rows: lambda^(steps to the chunk's end) in time's direction, 0 behind the sequence's end
+__device__ __forceinline__ void k_weights(float *wk, uint32_t *wk1, uint32_t *wk2, float ld, float sum_scale, int rows, bool back, int lane)
+{
+#pragma unroll 1
+    for (int i = lane; i < C / 2; i += 32) {
+        float w[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) w[e] = 2 * i + e < rows ? sum_scale * la_power(ld, back ? 2 * i + e : rows - 1 - 2 * i - e) : 0.0f;
+        wk[2 * i] = w[0];
+        wk[2 * i + 1] = w[1];
+        const uint32_t w1 = pack_bf16x2(w[0], w[1]);
+        wk1[i] = w1;
+        wk2[i] = narrow(add2(pair(w[0], w[1]), wide_negative(w1)));
+    }
+}
+// 32 columns of K over 16 N steps, weighted and transposed, as three bf16 pieces: two into tensor memory (`to`, and 64 columns on), the third into
+// `low`, which k_low() puts where K was
+template <int N>
+__device__ __forceinline__ void k_pieces3(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const float *wk, int lane, uint32_t (&low)[N][2][4])
+{
+    const f2 *w = reinterpret_cast<const f2 *>(wk) + (lane & 3), minus = pair(-1.0f, -1.0f);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const f2 ww[2] = {w[8 * j], w[8 * j + 4]};
+#pragma unroll
+        for (int g = 0; g < 2; ++g) ldsm4_t(from + (uint32_t)(j * 2048) + shift[g], low[j][g]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            uint32_t h[4], m[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f2 y = mul2(wide(low[j][g][e]), ww[e >> 1]);
+                h[e] = narrow(y);
+                y = fma2(wide(h[e]), minus, y);
+                m[e] = narrow(y);
+                low[j][g][e] = narrow(fma2(wide(m[e]), minus, y));
+            }
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 8 * j, h);
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64 + 8 * j, m);
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void k_low(uint32_t from, const uint32_t (&shift)[2], const uint32_t (&low)[N][2][4])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) stsm4_t(from + (uint32_t)(j * 2048) + shift[g], low[j][g]);
+    fence_proxy_async_smem();
+}
+// The same as two pieces, by bf16 arithmetic: k w1 = h + t exactly (8 by 8 bits), t + k w2 rounded once
+__device__ __forceinline__ void k_pieces2(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const uint32_t *wk1, const uint32_t *wk2, int lane, int steps)
+{
+    int i = lane & 3;
+#pragma unroll 1
+    for (int j = 0; j < steps; j += 16, from += 2048, to += 8, i += 8) {
+        const __nv_bfloat162 w1[2] = {as_bf2(wk1[i]), as_bf2(wk1[i + 4])}, w2[2] = {as_bf2(wk2[i]), as_bf2(wk2[i + 4])};
+        uint32_t k[2][4];
+        ldsm4_t(from + shift[0], k[0]);
+        ldsm4_t(from + shift[1], k[1]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            uint32_t h[4], m[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 kk = as_bf2(k[g][e]), hh = __hmul2(kk, w1[e >> 1]);
+                h[e] = as_word(hh);
+                m[e] = as_word(__hfma2(kk, w2[e >> 1], __hfma2(kk, w1[e >> 1], __hneg2(hh))));
+            }
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16), h);
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64, m);
+        }
+    }
+}
+
+// a role's place in the ring of chunks
+struct Place {
+    int at = 0;
+    uint32_t par = 0;
+    __device__ __forceinline__ bool next(Shared &sh, Chunk &c, bool on)
+    {
+        if (!on || !warp_wait(sh, &sh.told[at], par)) return false;
+        c = sh.chunk[at];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.heard[at]);
+        if (++at == RING) { at = 0; par ^= 1u; }
+        return (c.flags & END) == 0;
+    }
+};
+
 constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(C >> 4) << 24);      // fp32 sums of bf16, M = 128
 
-template <int DK, int DV, bool OUT>
+template <int DK, int DV>
 struct Layout {
-    static constexpr uint32_t Q = 0, K = OUT ? C * DK * 2 : 0, V = K + C * DK * 2, STAGE = V + C * DV * 2;
-    static constexpr uint32_t S_BYTES = OUT ? DK * DV * 2 : 0;
+    static constexpr uint32_t Q = 0, K = C * DK * 2, V = K + C * DK * 2, STAGE = V + C * DV * 2, S_BYTES = DK * DV * 2;
     static constexpr int ROOM = 224 * 1024 - (int)S_BYTES;
     static constexpr int STAGES = ROOM / (int)STAGE > 4 ? 4 : ROOM / (int)STAGE;
     static constexpr uint32_t CTL = S_BYTES + STAGES * STAGE;            // then the barriers and tables
@@ -159,52 +330,82 @@ struct Layout {
     static_assert(STAGES >= 2 && SMEM <= 227 * 1024, "two stages at least");
 };
 
-// OUT: outputs; without, the segments' own states, from zero, into `carry`
-template <int DK, int DV, bool OUT>
+template <int DK, int DV>
 __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Params p)
 {
-    using L = Layout<DK, DV, OUT>;
+    using L = Layout<DK, DV>;
     extern __shared__ __align__(1024) uint8_t base[];
     Shared &sh = *reinterpret_cast<Shared *>(base + L::CTL);
     const uint32_t s_smem = smem_u32(base), ring = s_smem + L::S_BYTES;
-    const int tid = threadIdx.x, group = tid >> 7, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
+    const int tid = threadIdx.x, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
     if (tid == 0) {
         for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < RING; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.heard[i], ROLE_WARPS); }
         mbar_init(&sh.sc_full, 1); mbar_init(&sh.qs_done, 1); mbar_init(&sh.u_full, 1); mbar_init(&sh.o_full, 1);
-        mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 4); mbar_init(&sh.low_ready, 4); mbar_init(&sh.s_ready, 4);
-        mbar_init(&sh.u_free, 4); mbar_init(&sh.o_scaled, 4); mbar_init(&sh.o_free, 4);
+        mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.s_ready, 8);
+        mbar_init(&sh.u_free, 8); mbar_init(&sh.o_scaled, 4); mbar_init(&sh.o_free, 4);
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 4 * (GROUPS - 1)) tmem_alloc(&sh.tmem, 512);
+    if (warp == 12) tmem_alloc(&sh.tmem, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tm = sh.tmem, lanes = tm + ((uint32_t)(quad * 32) << 16);
-    // every role goes through the same units and chunks
-    auto unit = [&](long long u, Unit &x) { return get_unit(p, u, x) && (OUT || !x.last); };
-    // 640 threads x 96 registers = 128 x (72 + 88 + 208 + 72 + 40)
-    if (group == 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (warp == 16) {
+    if (warp >= 12) {
+        if (warp == 12) {
             // ---------------------------------------------------------------- loads
-            int stage = 0;
-            uint32_t par = 1;
+            int stage = 0, slot = 0;
+            uint32_t par = 1, heard_par = 1;
             bool on = true;
-            for (long long u = blockIdx.x; u < p.units && on; u += gridDim.x) {
+            auto tell = [&](const Chunk &c) {
+                on = warp_wait(sh, &sh.heard[slot], heard_par);
+                if (!on) return;
+                if (lane == 0) {
+                    sh.chunk[slot] = c;
+                    mbar_arrive(&sh.told[slot]);
+                }
+                if (++slot == RING) { slot = 0; heard_par ^= 1u; }
+            };
+            Chunk k{};
+            for (int u = blockIdx.x; u < p.units && on; u += gridDim.x) {
                 Unit x;
-                if (!unit(u, x)) continue;
-                const int back = p.job[x.job].back, b = p.seqs.cu == nullptr ? x.seq : 0;
+                if (!get_unit(p, u, x)) continue;
+                const LaJob &job = p.job[x.job];
+                const int b = p.seqs.cu == nullptr ? x.seq : 0, size = job.Dk * job.Dv;
+                const size_t state = ((size_t)x.seq * p.seqs.H + x.h) * size;
+                float *const carry = p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * size;
+                k.job = x.job;
+                k.ld = p.seqs.log_decay[x.h];
+                k.sum_scale = job.sum_scale;
+                k.last = job.back && x.n > 0 ? la_power(k.ld, 1) : 1.0f;
+                k.from = x.c0 > 0 ? carry : job.s0 != nullptr ? job.s0 + state : nullptr;
+                k.turned = x.c0 == 0 && job.turned;
+                const int same = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (k.ld >= -44.0f / MID ? WEAK : 0);
+                __nv_bfloat16 *const out = (__nv_bfloat16 *)job.o.data + b * job.o.batch + x.h * job.o.head;
+                float *const to = x.last && job.s1 != nullptr ? job.s1 + state : nullptr;
+                if (x.c0 == x.c1) {
+                    k.flags = same | FIRST | LAST | NONE;
+                    k.rows = 0;
+                    k.to = to;
+                    tell(k);
+                    continue;
+                }
                 for (int c = x.c0; c < x.c1 && on; ++c) {
-                    const int rows = min(C, x.n - c * C);
-                    const int t = (int)x.start + (back ? x.n - c * C - rows : c * C);
-                    on = warp_wait(sh, &sh.empty[stage], par);
+                    const bool first = c == x.c0, last = c + 1 == x.c1;
+                    k.rows = min(C, x.n - c * C);
+                    const int t = (int)x.start + (job.back ? x.n - c * C - k.rows : c * C);
+                    k.flags = same | (first ? FIRST : 0) | (last ? LAST : 0) | (!first || k.from != nullptr ? STATE : 0) | (c == 0 && job.back ? 0 : LATE);
+                    k.out = out + (long long)t * job.o.token;
+                    k.to = last ? to : nullptr;
+                    tell(k);
+                    if (on) on = warp_wait(sh, &sh.empty[stage], par);
                     if (!on) break;
                     if (elect_one()) {
                         const uint32_t at = ring + (uint32_t)stage * L::STAGE;
                         mbar_expect_tx(&sh.full[stage], L::STAGE);
 #pragma unroll
-                        for (int r = OUT ? 0 : 1; r < 3; ++r) {
+                        for (int r = 0; r < 3; ++r) {
                             const int m = p.which[x.job][r], hh = p.flat[m] & 2 ? 0 : x.h, bb = p.flat[m] & 1 ? 0 : b;
                             const uint32_t to = at + (r == 0 ? L::Q : r == 1 ? L::K : L::V);
 #pragma unroll
@@ -216,368 +417,349 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
                 }
             }
-        } else if (warp == 17) {
+            k.flags = END;
+            if (on) tell(k);
+        } else {
             // ---------------------------------------------------------------- products
             int stage = 0;
-            uint32_t full_par = 0, par = 0, s_par = 0, low_par = 0;        // par: barriers that complete once a chunk
+            uint32_t full_par = 0, par = 0, s_par = 0, o_par = 0;          // par: barriers that complete once a chunk
             bool on = true, first = true;
+            const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0);            // (known to the compiler as the same in all lanes)
             auto wait = [&](uint64_t *bar, uint32_t parity) {
                 if (on) on = warp_wait(sh, bar, parity);
                 tc_fence_after();
             };
-            for (long long u = blockIdx.x; u < p.units && on; u += gridDim.x) {
-                Unit x;
-                if (!unit(u, x)) continue;
-                const LaJob &job = p.job[x.job];
-                const bool init = OUT && (x.c0 > 0 || job.s0 != nullptr), three = !OUT || job.s1 != nullptr;
-                const uint32_t ik = IDESC | ((uint32_t)(C >> 3) << 17), iv = IDESC | (1u << 16) | ((uint32_t)(job.Dv >> 3) << 17);
-                const int nk = job.Dk / 16;
-                for (int c = x.c0; c < x.c1 && on; ++c) {
-                    const uint32_t at = ring + (uint32_t)stage * L::STAGE;
-                    const uint64_t vd = desc_mn(at + L::V, C * 128);
-                    const bool state = OUT && (c > x.c0 || init);
-                    // columns of tensor memory by K' pieces (or P) times V
-                    auto times_v = [&](uint32_t d, uint32_t a, bool add) {
-#pragma unroll 1
-                        for (int k = 0; k < C / 16; ++k) umma_ts(tm + d, tm + a + 8 * k, vd + (uint64_t)k * (2048 >> 4), iv, add || k > 0);
-                    };
-                    wait(&sh.full[stage], full_par);
-                    if (OUT && on && elect_one()) {
-                        uint64_t qd = smem_desc_sw128(at + L::Q), kd = smem_desc_sw128(at + L::K);
-#pragma unroll 1
-                        for (int k = 0; k < nk; ++k) {
-                            umma_bf16(tm + COL_SC, qd, kd, ik, k > 0);
-                            const uint64_t step = (k & 3) == 3 ? (C * 128 - 96) >> 4 : 2;     // 16 values on, or the next panel
-                            qd += step;
-                            kd += step;
-                        }
-                        umma_commit(&sh.sc_full);
-                    }
-                    __syncwarp();
-                    if (OUT && !first) wait(&sh.o_free, par ^ 1u);
-                    if (state) {
-                        wait(&sh.s_ready, s_par);
-                        if (on && elect_one()) {
-                            uint64_t qd = smem_desc_sw128(at + L::Q), sd = desc_mn(s_smem, DK * 128);
-#pragma unroll 1
-                            for (int k = 0; k < nk; ++k) {
-                                umma_bf16(tm + COL_O, qd, sd, iv, k > 0);
-                                qd += (k & 3) == 3 ? (C * 128 - 96) >> 4 : 2;
-                                sd += 2048 >> 4;
-                            }
-                            umma_commit(&sh.qs_done);
-                        }
-                        __syncwarp();
-                    }
-                    wait(&sh.k_ready, par);
-                    if (!first) wait(&sh.u_free, par ^ 1u);
-                    if (on && elect_one()) {
-                        times_v(COL_U, COL_K + 64, false);
-                        times_v(COL_U, COL_K, true);
-                        if (!three) umma_commit(&sh.u_full);
-                    }
-                    __syncwarp();
-                    if (OUT) wait(&sh.p_ready, par);
-                    if (three) {
-                        wait(&sh.low_ready, low_par);
-                        low_par ^= 1u;
-                        if (on && elect_one()) {
-                            times_v(COL_U, COL_LOW, true);
-                            umma_commit(&sh.u_full);
-                        }
-                        __syncwarp();
-                    }
-                    if (OUT) {
-                        if (state) {
-                            wait(&sh.o_scaled, s_par);
-                            s_par ^= 1u;
-                        }
-                        if (on && elect_one()) {
-                            times_v(COL_O, COL_SC, state);
-                            umma_commit(&sh.o_full);
-                        }
-                        __syncwarp();
-                    }
-                    if (on && elect_one()) umma_commit(&sh.empty[stage]);
-                    __syncwarp();
-                    if (++stage == L::STAGES) { stage = 0; full_par ^= 1u; }
-                    par ^= 1u;
-                    first = false;
-                }
-            }
-        }
-    } else if (group == 0) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        // -------------------------------------------------------------------- P
-        uint32_t par = 0;
-        bool on = true;
-        for (long long u = blockIdx.x; OUT && u < p.units && on; u += gridDim.x) {
-            Unit x;
-            if (!unit(u, x)) continue;
-            const LaJob &job = p.job[x.job];
-            const bool back = job.back != 0;
-            const float ld = p.seqs.log_decay[x.h];
-            // weights of a block's columns against its last one, backwards against its first one
-            float *const near = sh.near[quad];
-            __syncwarp();
-            near[lane] = la_power(ld, back ? lane : 31 - lane);
-            __syncwarp();
-            for (int c = x.c0; c < x.c1; ++c, par ^= 1u) {
-                const int rows = min(C, x.n - c * C);
-                on = warp_wait(sh, &sh.sc_full, par);
-                if (!on) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int b = 0; b < 4; ++b) {
-                    uint32_t w[16];
-                    if (back ? b < quad : b > quad) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = 0u;
-                    } else {
-                        float s[32];
-                        tmem_ld32(lanes + COL_SC + 32 * b, s);
-                        if (b != quad) {
-                            // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
-                            const float f = job.sum_scale * la_power(ld, back ? 32 * b - row : row - 32 * b - 31);
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 r = *reinterpret_cast<const float4 *>(&near[e]);
-                                s[e] *= f * r.x; s[e + 1] *= f * r.y; s[e + 2] *= f * r.z; s[e + 3] *= f * r.w;
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const int far = back ? e - lane : lane - e;
-                                s[e] = far >= 0 ? s[e] * (job.sum_scale * near[back ? max(far, 0) : 31 - max(far, 0)]) : 0.0f;
-                            }
-                        }
-                        if (32 * b + 32 > rows) {                                  // steps behind the sequence's end, whatever lies there
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) s[e] = 32 * b + e < rows ? s[e] : 0.0f;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
-                    }
-                    tmem_st16(lanes + COL_SC + 16 * b, w);
-                }
-                tmem_wait_st();
-                tmem_arrive(&sh.p_ready);
-            }
-        }
-    } else if (group == 1) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        // -------------------------------------------------------------------- K
-        int stage = 0;
-        uint32_t full_par = 0, par = 0;
-        bool on = true, first = true;
-        for (long long u = blockIdx.x; u < p.units && on; u += gridDim.x) {
-            Unit x;
-            if (!unit(u, x)) continue;
-            const LaJob &job = p.job[x.job];
-            const float ld = p.seqs.log_decay[x.h];
-            const bool three = !OUT || job.s1 != nullptr;
-            int had = 0;                                                           // rows that the weights in shared memory are for
-            for (int c = x.c0; c < x.c1; ++c) {
-                const int rows = min(C, x.n - c * C);
-                if (rows != had) {
-                    __syncwarp();
-#pragma unroll
-                    for (int j = lane; j < C; j += 32) sh.wk[quad][j] = j < rows ? job.sum_scale * la_power(ld, job.back ? j : rows - 1 - j) : 0.0f;
-                    __syncwarp();
-                    had = rows;
-                }
+            Place place;
+            Chunk ch;
+            while (place.next(sh, ch, on)) {
+                const int flags = __shfl_sync(0xffffffffu, ch.flags, 0), job = __shfl_sync(0xffffffffu, ch.job, 0);
+                if (flags & NONE) continue;
+                const bool state = flags & STATE;
+                const uint32_t ik = IDESC | ((uint32_t)(C >> 3) << 17), iv = IDESC | (1u << 16) | ((uint32_t)(p.job[job].Dv >> 3) << 17);
+                const int nk = p.job[job].Dk / 16;
                 const uint32_t at = ring + (uint32_t)stage * L::STAGE;
-                on = warp_wait(sh, &sh.full[stage], full_par);
-                if (on && !first) on = warp_wait(sh, &sh.u_full, par ^ 1u);          // the pieces before these have been multiplied
-                if (!on) break;
-                tc_fence_after();
-                if (row >= rows) {                                                 // steps behind the sequence's end: zeros in V
+                const uint64_t vd = desc_mn(at + L::V, C * 128);
+                constexpr uint64_t K16 = 2048 >> 4;                                // sixteen rows of an operand with N (or M) together
+                // columns of tensor memory by K's pieces (or P) times V
+                auto times_v = [&](uint32_t d, uint32_t a, bool add) {
 #pragma unroll
-                    for (int d = 0; d < DV / 64; ++d)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sts128(at + L::V + (uint32_t)(d * C * 128 + row * 128 + e * 16), 0, 0, 0, 0);
-                    fence_proxy_async_smem();
-                }
-                const uint32_t col = at + L::K + (uint32_t)((row >> 6) * (C * 128) + (row & 7) * 2), piece = (uint32_t)(row >> 3) & 7u;
-                // sixteen steps at a time; `which`: the upper two pieces or the third
-                auto cut = [&](bool upper) {
-#pragma unroll 1
-                    for (int j0 = 0; j0 < C; j0 += 16) {
-                        uint32_t h[8], m[8], l[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int j = j0 + 2 * e;
-                            const float2 w = *reinterpret_cast<const float2 *>(&sh.wk[quad][j]);
-                            float a = lds_bf16(col + (uint32_t)(j * 128) + ((piece ^ (uint32_t)(j & 7)) << 4)) * w.x;
-                            float b = lds_bf16(col + (uint32_t)((j + 1) * 128) + ((piece ^ (uint32_t)((j + 1) & 7)) << 4)) * w.y;
-                            if (rows < C) {
-                                a = j < rows ? a : 0.0f;
-                                b = j + 1 < rows ? b : 0.0f;
-                            }
-                            h[e] = pack_bf16x2(a, b);
-                            a -= __uint_as_float(h[e] << 16);
-                            b -= __uint_as_float(h[e] & 0xffff0000u);
-                            m[e] = pack_bf16x2(a, b);
-                            a -= __uint_as_float(m[e] << 16);
-                            b -= __uint_as_float(m[e] & 0xffff0000u);
-                            l[e] = pack_bf16x2(a, b);
-                        }
-                        if (upper) {
-                            tmem_st8(lanes + COL_K + (uint32_t)(j0 / 2), h);
-                            tmem_st8(lanes + COL_K + 64 + (uint32_t)(j0 / 2), m);
-                        } else tmem_st8(lanes + COL_LOW + (uint32_t)(j0 / 2), l);
-                    }
-                    tmem_wait_st();
+                    for (int k = 0; k < C / 16; ++k) umma_ts(tmu + d, tmu + a + 8 * k, vd + k * K16, iv, add || k > 0);
                 };
-                if (quad * 32 < DK) cut(true);
-                tmem_arrive(&sh.k_ready);
-                // the scores that lie where the third piece goes have been read (a barrier is waited for in every chunk or in none:
-                // one that is two phases behind looks as if it had completed)
-                if (OUT) on = warp_wait(sh, &sh.p_ready, par);
-                if (!on) break;
-                if (three) {
-                    tc_fence_after();
-                    if (quad * 32 < DK) cut(false);
-                    tmem_arrive(&sh.low_ready);
+                // Q (its rows' values together) times the operand whose descriptor of step k is b(k)
+                auto q_times = [&](uint32_t d, uint32_t idesc, auto b) {
+                    const uint64_t qd = smem_desc_sw128(at + L::Q);
+#pragma unroll
+                    for (int k = 0; k < DK / 16; ++k)
+                        if (k < nk) umma_bf16(tmu + d, qd + (uint64_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2), b(k), idesc, k > 0);
+                };
+                wait(&sh.full[stage], full_par);
+                if (on && elect_one()) {
+                    const uint64_t kd = smem_desc_sw128(at + L::K);
+                    q_times(COL_SC, ik, [&](int k) { return kd + (uint64_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2); });
+                    umma_commit(&sh.sc_full);
                 }
+                __syncwarp();
+                wait(&sh.k_ready, par);
+                if (!first) wait(&sh.u_free, par ^ 1u);
+                if (on && elect_one()) {
+                    // the small pieces first, while the sum is small: it is rounded towards zero at every step
+                    if (flags & THREE) {
+                        const uint64_t kd = desc_mn(at + L::K, C * 128);
+#pragma unroll
+                        for (int k = 0; k < C / 16; ++k) umma_bf16(tmu + COL_U, kd + k * K16, vd + k * K16, iv | (1u << 15), k > 0);
+                    }
+                    times_v(COL_U, COL_K + 64, flags & THREE);
+                    times_v(COL_U, COL_K, true);
+                    umma_commit(&sh.u_full);
+                }
+                __syncwarp();
+                if (!first) wait(&sh.o_free, par ^ 1u);
+                if (state) {
+                    wait(&sh.s_ready, s_par);
+                    s_par ^= 1u;
+                    if (on && elect_one()) {
+                        const uint64_t sd = desc_mn(s_smem, DK * 128);
+                        q_times(COL_O, iv, [&](int k) { return sd + k * K16; });
+                        umma_commit(&sh.qs_done);
+                    }
+                    __syncwarp();
+                }
+                wait(&sh.p_ready, par);
+                if (state && !(flags & WEAK)) {
+                    wait(&sh.o_scaled, o_par);
+                    o_par ^= 1u;
+                }
+                if (on && elect_one()) {
+                    times_v(COL_O, COL_SC, state);
+                    umma_commit(&sh.o_full);
+                }
+                __syncwarp();
+                if (on && elect_one()) umma_commit(&sh.empty[stage]);
+                __syncwarp();
                 if (++stage == L::STAGES) { stage = 0; full_par ^= 1u; }
                 par ^= 1u;
                 first = false;
             }
         }
-    } else if (group == 2) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        // -------------------------------------------------------------------- S
-        uint32_t par = 0, qs_par = 1;
-        bool on = true, wrote = false;
-        const bool mine = row < DK;
-        for (long long u = blockIdx.x; u < p.units; u += gridDim.x) {
-            Unit x;
-            if (!unit(u, x)) continue;
-            const LaJob &job = p.job[x.job];
-            const float ld = p.seqs.log_decay[x.h];
-            const int Dk = job.Dk, Dv = job.Dv;
-            const bool have = mine && row < Dk;
-            float S[DV];
-#pragma unroll
-            for (int v = 0; v < DV; ++v) S[v] = 0.0f;
-            const size_t at = ((size_t)x.seq * p.seqs.H + x.h) * Dk * Dv;
-            float *const carry = p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * Dk * Dv + (size_t)row * Dv;
-            const float *const from = !OUT ? nullptr : x.c0 > 0 ? carry : job.s0;
-            if (from != nullptr && have) {
-                if (x.c0 == 0 && job.turned) {
-#pragma unroll
-                    for (int v = 0; v < DV; ++v)
-                        if (v < Dv) S[v] = from[at + (size_t)v * Dk + row];
-                } else {
-                    const float *r = x.c0 > 0 ? from : from + at + (size_t)row * Dv;
-#pragma unroll
-                    for (int v = 0; v < DV; v += 4)
-                        if (v < Dv) {
-                            const float4 y = *reinterpret_cast<const float4 *>(r + v);
-                            S[v] = y.x; S[v + 1] = y.y; S[v + 2] = y.z; S[v + 3] = y.w;
-                        }
-                }
-            }
-            // the state to shared memory, in bf16, for Q S
-            auto hand_over = [&]() {
-                if (on && wrote) on = warp_wait(sh, &sh.qs_done, qs_par);            // the product with the one before is done
-                wrote = true;
-                qs_par ^= 1u;
-                if (mine) {
-#pragma unroll
-                    for (int v = 0; v < DV; v += 8)
-                        sts128(s_smem + (uint32_t)((v >> 6) * (DK * 128) + row * 128 + ((((v & 63) >> 3) ^ (row & 7)) << 4)), pack_bf16x2(S[v], S[v + 1]),
-                               pack_bf16x2(S[v + 2], S[v + 3]), pack_bf16x2(S[v + 4], S[v + 5]), pack_bf16x2(S[v + 6], S[v + 7]));
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.s_ready);
-            };
-            if (from != nullptr && x.c1 > x.c0) hand_over();
-            for (int c = x.c0; c < x.c1; ++c) {
-                const int rows = min(C, x.n - c * C);
-                const LaStep step(ld, rows - 1 + (c == 0 && job.back ? 0 : 1));
-                if (on) on = warp_wait(sh, &sh.u_full, par);
-                par ^= 1u;
-                if (!on) break;
-                tc_fence_after();
-                if (mine) {
-#pragma unroll
-                    for (int v = 0; v < DV; v += 32) {
-                        float U[32];
-                        tmem_ld32(lanes + COL_U + v, U);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) S[v + e] = step(S[v + e], U[e]);
-                    }
-                }
-                tmem_arrive(&sh.u_free);
-                if (OUT && c + 1 < x.c1) hand_over();
-            }
-            float *const to = !OUT ? carry : x.last && job.s1 != nullptr ? job.s1 + at + (size_t)row * Dv : nullptr;
-            if (to != nullptr && have) {
-                const float f = !on ? NAN : OUT && job.back && x.n > 0 ? la_power(ld, 1) : 1.0f;
-#pragma unroll
-                for (int v = 0; v < DV; v += 4)
-                    if (v < Dv) *reinterpret_cast<float4 *>(to + v) = make_float4(f * S[v], f * S[v + 1], f * S[v + 2], f * S[v + 3]);
-            }
-        }
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        // -------------------------------------------------------------------- O
-        uint32_t par = 0, s_par = 0;
+    } else if (warp < 4) {
+        // ------------------------------------------------------------- P, and O of the chunk before
+        uint32_t par = 0, qs_par = 0;
         bool on = true;
-        for (long long u = blockIdx.x; OUT && u < p.units; u += gridDim.x) {
-            Unit x;
-            if (!unit(u, x)) continue;
-            const LaJob &job = p.job[x.job];
-            const float ld = p.seqs.log_decay[x.h];
-            const bool init = x.c0 > 0 || job.s0 != nullptr;
-            const int b = p.seqs.cu == nullptr ? x.seq : 0, Dv = job.Dv;
-            __nv_bfloat16 *const o = (__nv_bfloat16 *)job.o.data + b * job.o.batch + x.start * job.o.token + x.h * job.o.head;
-            for (int c = x.c0; c < x.c1; ++c) {
-                const int rows = min(C, x.n - c * C);
-                if (c > x.c0 || init) {
-                    const int late = c == 0 && job.back ? 0 : 1;
-                    const float f = la_power(ld, max(job.back ? rows - 1 - row : row, 0) + late);
-                    if (on) on = warp_wait(sh, &sh.qs_done, s_par);
-                    s_par ^= 1u;
-                    if (on) {
-                        tc_fence_after();
+        // a chunk whose sum is still to go out
+        __nv_bfloat16 *out = nullptr;
+        float out_f = 0.0f;
+        int out_rows = 0, out_dv = 0;
+        bool due = false;
+        auto put_out = [&]() {
+            if (on) on = warp_wait(sh, &sh.o_full, par ^ 1u);
+            tc_fence_after();
+            const f2 ff = pair(out_f, out_f);
+            const bool in = row < out_rows;
 #pragma unroll 1
-                        for (int v = 0; v < Dv; v += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(lanes + COL_O + v, r);
-                            tmem_wait_ld();
+            for (int v = 0; v < out_dv; v += 64) {                                 // (columns beyond Dv hold something or other)
+                uint32_t r[32], q[32];
+                tmem_ld32_issue(lanes + COL_O + v, r);
+                tmem_ld32_issue(lanes + COL_O + v + 32, q);
+                tmem_wait_ld();
+                if (on && v + 64 >= out_dv) tmem_arrive(&sh.o_free);               // (before the last stores: the next sum may come)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-                            tmem_st16(lanes + COL_O + v, r);
+                for (int e = 0; e < 16; ++e) {
+                    r[e] = narrow(mul2(pair(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), ff));
+                    q[e] = narrow(mul2(pair(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1])), ff));
+                }
+                if (!on)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[e] = q[e] = 0x7fff7fffu;        // a wait gave up: NaN
+                if (in) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (v + 8 * e < out_dv) *reinterpret_cast<uint4 *>(out + v + 8 * e) = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (v + 32 + 8 * e < out_dv) *reinterpret_cast<uint4 *>(out + v + 32 + 8 * e) = make_uint4(q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]);
+                }
+            }
+        };
+        Place place;
+        Chunk ch;
+        int had = -1;                                                              // rows (and more) that the table is for
+        while (place.next(sh, ch, true)) {
+            if (ch.flags & NONE) continue;
+            const bool back = ch.flags & BACK, weak = ch.flags & WEAK;
+            const int rows = ch.rows, late = ch.flags & LATE ? 1 : 0;
+            if (due) put_out();
+            if (on) on = warp_wait(sh, &sh.sc_full, par);
+            if (on) {
+                tc_fence_after();
+                if ((ch.flags & FIRST) || had != 2 * rows + late) {
+                    had = 2 * rows + late;
+                    if (weak) {
+#pragma unroll 1
+                        for (int j = lane; j < C; j += 32) sh.wp[j] = ch.sum_scale * power_of(ch.ld, MID - (back ? rows - 1 - j : j) - late);
+                    } else sh.wp[lane] = ch.sum_scale * la_power(ch.ld, back ? lane : 31 - lane);
+                    __syncwarp();
+                }
+                // Columns of block b that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
+                auto kept = [&](int b) -> uint32_t {
+                    const uint32_t own = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                    const int there = rows - 32 * b;
+                    return (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) & (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
+                };
+                const int b0 = back ? quad : 0, b1 = back ? 4 : quad + 1;          // blocks with anything in them
+                if (weak) {
+#pragma unroll 1
+                    for (int b = 0; b < 4; b += 2) {                               // (two blocks' scores on their way at a time)
+                        uint32_t s[32], t[32], w[16];
+                        tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
+                        tmem_ld32_issue(lanes + COL_SC + 32 * b + 32, t);
+                        tmem_wait_ld();
+                        p_pack(s, w, sh.wp + 32 * b, kept(b));
+                        tmem_st16(lanes + COL_SC + 16 * b, w);
+                        p_pack(t, w, sh.wp + 32 * b + 32, kept(b + 1));
+                        tmem_st16(lanes + COL_SC + 16 * b + 16, w);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t s[32], w[16];
+                        tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
+                        tmem_wait_ld();
+                        if (b != quad) {
+                            // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
+                            const float f = b >= b0 && b < b1 ? la_power(ch.ld, back ? 32 * b - row : row - 32 * b - 31) : 0.0f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
+                            p_pack(s, w, sh.wp, kept(b));
+                        } else {
+                            // the row's own block: the power of the distance
+                            const uint32_t keep = kept(b);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const int far = max(back ? e - lane : lane - e, 0);
+                                s[e] = keep >> e & 1u ? __float_as_uint(__uint_as_float(s[e]) * sh.wp[back ? far : 31 - far]) : 0u;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
                         }
-                        tmem_wait_st();
-                        tmem_arrive(&sh.o_scaled);
+                        tmem_st16(lanes + COL_SC + 16 * b, w);
                     }
                 }
-                if (on) on = warp_wait(sh, &sh.o_full, par);
-                par ^= 1u;
-                tc_fence_after();
-                __nv_bfloat16 *const to = o + (long long)((job.back ? x.n - c * C - rows : c * C) + row) * job.o.token;
+                tmem_wait_st();
+                tmem_arrive(&sh.p_ready);
+            }
+            const LaJob &job = p.job[ch.job];
+            const int pos = (back ? rows - 1 - row : row) + late;
+            const bool in = row < rows;
+            if (ch.flags & STATE) {
+                // (a barrier is waited for in every one of its phases: one that is two phases behind looks as if it had completed)
+                if (on) on = warp_wait(sh, &sh.qs_done, qs_par);
+                qs_par ^= 1u;
+                if (on && !weak) {
+                    const float g = in ? la_power(ch.ld, pos) : 0.0f;
+                    tc_fence_after();
 #pragma unroll 1
-                for (int v = 0; v < Dv; v += 16) {
-                    uint32_t r[16];
-                    if (on) {
+                    for (int v = 0; v < job.Dv; v += 16) {
+                        uint32_t r[16];
                         tmem_ld16(lanes + COL_O + v, r);
                         tmem_wait_ld();
-                    }
-                    uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        w[e] = on ? pack_bf16x2(__uint_as_float(r[2 * e]) * job.out_scale, __uint_as_float(r[2 * e + 1]) * job.out_scale) : 0x7fff7fffu;
-                    if (row < rows) {
-                        *reinterpret_cast<uint4 *>(to + v) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4 *>(to + v + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                        for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
+                        tmem_st16(lanes + COL_O + v, r);
+                    }
+                    tmem_wait_st();
+                    tmem_arrive(&sh.o_scaled);
+                }
+            }
+            out = ch.out + (long long)row * job.o.token;
+            out_f = job.out_scale * (!weak ? 1.0f : in ? power_of(ch.ld, pos - MID) : 0.0f);
+            out_rows = rows;
+            out_dv = job.Dv;
+            due = true;
+            par ^= 1u;
+        }
+        if (due) put_out();
+    } else {
+        // ------------------------------------------------------------- K and S
+        int stage = 0;
+        uint32_t full_par = 0, par = 0, qs_par = 1;
+        bool on = true, wrote = false;
+        const int half = (warp - 4) >> 2;                                          // of a chunk's steps and of the state's columns
+        constexpr int HV = DV / 2, HC = C / 2;
+        const bool mine = row < DK;
+        const int v0 = half * HV;
+        // this warp's 32 columns of K: panel, first 16 bytes of a row there; lane i reads row i % 8 of block i / 8, steps in the upper bit of
+        // the block's number, columns in the lower
+        const uint32_t piece = (uint32_t)(quad & 1) * 4, panel0 = ring + L::K + (uint32_t)((quad >> 1) * (C * 128));
+        const uint32_t from = (uint32_t)((half * HC + ((lane >> 4) << 3) + (lane & 7)) * 128);
+        const uint32_t shift[2] = {((piece + ((lane >> 3) & 1)) ^ (uint32_t)(lane & 7)) << 4, ((piece + 2 + ((lane >> 3) & 1)) ^ (uint32_t)(lane & 7)) << 4};
+        const uint32_t k_to = lanes + COL_K + (uint32_t)(half * HC / 2);
+        const uint32_t s_row = s_smem + (uint32_t)((v0 >> 6) * (DK * 128) + row * 128), s_turn = (uint32_t)(row & 7) << 4;
+        f2 S[HV / 2];
+        Place place;
+        Chunk ch;
+        int had = 0;                                                               // rows that the tables are for
+        while (place.next(sh, ch, true)) {
+            const int Dk = p.job[ch.job].Dk, Dv = p.job[ch.job].Dv, rows = ch.rows;
+            const bool have = mine && row < Dk;
+            if (ch.flags & FIRST) {
+#pragma unroll
+                for (int v = 0; v < HV / 2; ++v) S[v] = 0;
+                if (ch.from != nullptr && have) {
+                    if (ch.turned) {
+                        const float *r = ch.from + row + v0 * Dk;
+#pragma unroll
+                        for (int v = 0; v < HV; v += 2)
+                            if (v0 + v < Dv) S[v / 2] = pair(r[v * Dk], r[(v + 1) * Dk]);
+                    } else {
+                        const float4 *r = reinterpret_cast<const float4 *>(ch.from + row * Dv + v0);
+#pragma unroll
+                        for (int v = 0; v < HV; v += 4)
+                            if (v0 + v < Dv) {
+                                const float4 y = r[v / 4];
+                                S[v / 2] = pair(y.x, y.y);
+                                S[v / 2 + 1] = pair(y.z, y.w);
+                            }
                     }
                 }
-                if (on) tmem_arrive(&sh.o_free);
+            }
+            if (!(ch.flags & NONE)) {
+                if (on) on = warp_wait(sh, &sh.full[stage], full_par);
+                if (on) {
+                    tc_fence_after();
+                    if ((ch.flags & FIRST) || rows != had) {                       // (this warp has seen the chunk before's products complete)
+                        had = rows;
+                        k_weights(sh.wk, sh.wk1, sh.wk2, ch.ld, ch.sum_scale, rows, ch.flags & BACK, lane);
+                        __syncwarp();
+                    }
+                    const uint32_t at = ring + (uint32_t)stage * L::STAGE, panel = panel0 + (uint32_t)stage * L::STAGE;
+                    if (rows < C) {                                                // steps behind the sequence's end: zeros, in V and in K
+                        if (half == 0 && row >= rows)
+#pragma unroll 1
+                            for (int d = 0; d < DV / 8; ++d) sts128(at + L::V + (uint32_t)((d >> 3) * (C * 128) + row * 128 + (d & 7) * 16), 0, 0, 0, 0);
+                        if (quad * 32 < DK)
+#pragma unroll 1
+                            for (int j = max(rows, half * HC) + (lane >> 2); j < (half + 1) * HC; j += 8)
+                                sts128(panel + (uint32_t)(j * 128) + (((piece + (uint32_t)(lane & 3)) ^ (uint32_t)(j & 7)) << 4), 0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    uint32_t low[HC / 16][2][4];
+                    if (quad * 32 < DK) {
+                        if (ch.flags & THREE) k_pieces3<HC / 16>(panel + from, shift, k_to, sh.wk + half * HC, lane, low);
+                        else k_pieces2(panel + from, shift, k_to, sh.wk1 + half * HC / 2, sh.wk2 + half * HC / 2, lane, HC);
+                        tmem_wait_st();
+                    }
+                    on = warp_wait(sh, &sh.sc_full, par);                          // K as it is has met Q: the third piece takes its place
+                    if (on && (ch.flags & THREE) && quad * 32 < DK) k_low<HC / 16>(panel + from, shift, low);
+                    if (on) tmem_arrive(&sh.k_ready);
+                }
+                if (ch.flags & STATE) {
+                    // the state before the chunk to shared memory, in bf16, for Q S
+                    if (on && wrote) on = warp_wait(sh, &sh.qs_done, qs_par);      // the product with the one before is done
+                    wrote = true;
+                    qs_par ^= 1u;
+                    const float mid = ch.flags & WEAK ? power_of(ch.ld, MID) : 1.0f;
+                    if (mine) {
+                        const f2 mm = pair(mid, mid);
+#pragma unroll
+                        for (int v = 0; v < HV; v += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) w[e] = narrow(mul2(S[v / 2 + e], mm));
+                            sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.s_ready);
+                }
+                const LaStep step(ch.ld, rows - 1 + (ch.flags & LATE ? 1 : 0));
+                if (on) on = warp_wait(sh, &sh.u_full, par);
+                par ^= 1u;
+                if (++stage == L::STAGES) { stage = 0; full_par ^= 1u; }
+                tc_fence_after();
+                if (mine && on) {
+                    const f2 w = pair(step.w, step.w), stay = pair(step.stay, step.stay);
+#pragma unroll
+                    for (int v = 0; v < HV; v += 32) {
+                        uint32_t U[32];
+                        tmem_ld32_issue(lanes + COL_U + v0 + v, U);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            f2 &y = S[v / 2 + e];
+                            y = fma2(stay, y, fma2(w, y, pair(__uint_as_float(U[2 * e]), __uint_as_float(U[2 * e + 1]))));
+                        }
+                    }
+                }
+                if (on) tmem_arrive(&sh.u_free);
+            }
+            if ((ch.flags & LAST) && ch.to != nullptr && have) {
+                const float f = on ? ch.last : NAN;
+                float4 *const to = reinterpret_cast<float4 *>(ch.to + row * Dv + v0);
+#pragma unroll
+                for (int v = 0; v < HV; v += 4)
+                    if (v0 + v < Dv) to[v / 4] = make_float4(f * lo(S[v / 2]), f * hi(S[v / 2]), f * lo(S[v / 2 + 1]), f * hi(S[v / 2 + 1]));
             }
         }
     }
@@ -587,53 +769,227 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     // After a wait that gave up: what is on its way (copies, MMAs), microseconds' worth, ends before shared and tensor memory are given back.
     if (sh.dead != 0)
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    if (warp == 4 * (GROUPS - 1)) {
+    if (warp == 12) {
         tc_fence_after();
         tmem_dealloc(tm, 512);
     }
 }
 
-// The segments' own states become the states that they start from: C_0 = S0, C_{i+1} = lambda^seg C_i + own_i.  A thread per value.
-__global__ void la_carry_kernel(const __grid_constant__ Params p)
+// ------------------------------------------------------------------ the segments' own states
+// From zero, of every segment but a sequence's last one, into `carry`: the K and S roles of the kernel above and nothing else, K's pieces and U
+// in two sets of tensor memory each, so that the sum of one chunk is taken up while the next one's is made.
+struct StateShared {
+    uint64_t full[4], empty[4], k_ready[2], u_full[2], u_free[2];
+    uint32_t tmem;
+    int dead;
+    alignas(16) float wk[4][C];              // a warp's own tables
+    uint32_t wk1[4][C / 2], wk2[4][C / 2];
+};
+constexpr int STATE_TH = 384;
+constexpr uint32_t STATE_U = 0, STATE_K = 256;
+
+template <int DK, int DV>
+__global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_constant__ Params p)
 {
-    const int job_i = blockIdx.z, h = blockIdx.x % p.seqs.H, seq = blockIdx.x / p.seqs.H;
-    const LaJob &job = p.job[job_i];
-    const int e = blockIdx.y * blockDim.x + threadIdx.x, size = job.Dk * job.Dv;
-    if (e >= size) return;
-    long long start, slot;
-    const int n = la_sequence(p.seqs, seq, start);
-    if (p.seqs.cu == nullptr) slot = (long long)seq * (p.slots / p.seqs.n);
-    else slot = min(max((long long)p.seqs.cu[seq], 0ll), p.seqs.T) / p.seg + seq;
-    const int d = e / job.Dv, v = e % job.Dv;
-    float S = 0.0f;
-    if (job.s0 != nullptr) S = job.s0[((size_t)seq * p.seqs.H + h) * size + (job.turned ? (size_t)v * job.Dk + d : (size_t)e)];
-    const float ld = p.seqs.log_decay[h];
-    float *c = p.carry + (((size_t)job_i * p.slots + slot) * p.seqs.H + h) * size + e;
-    const size_t next = (size_t)p.seqs.H * size;
-    int late = job.back ? 0 : 1;
-    for (long long at = 0; at < n; at += p.seg, c += next, late = 1) {
-        const bool more = at + p.seg < n;
-        const float own = more ? *c : 0.0f;
-        *c = S;
-        if (more) S = LaStep(ld, (int)p.seg - 1 + late)(S, own);
+    constexpr uint32_t V = C * DK * 2, STAGE = V + C * DV * 2;
+    constexpr int STAGES = 3;
+    extern __shared__ __align__(1024) uint8_t base[];
+    __shared__ StateShared sh;
+    const uint32_t ring = (smem_u32(base) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
+    if (tid == 0) {
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.k_ready[i], 4); mbar_init(&sh.u_full[i], 1); mbar_init(&sh.u_free[i], 4); }
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) tmem_alloc(&sh.tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = sh.tmem, lanes = tm + ((uint32_t)(quad * 32) << 16);
+    int stage = 0, g = 0;                                    // g: chunks so far
+    uint32_t full_par = 0;
+    bool on = true;
+    auto next = [&]() {
+        if (++stage == STAGES) { stage = 0; full_par ^= 1u; }
+        ++g;
+    };
+    // (after a wait that gave up the S role goes on alone and writes NaN)
+    for (int u = blockIdx.x; u < p.units && (on || (warp >> 2) == 1); u += gridDim.x) {
+        Unit x;
+        if (!get_unit(p, u, x) || x.last) continue;
+        const LaJob &job = p.job[x.job];
+        const bool back = job.back != 0, three = job.s1 != nullptr;
+        const float ld = p.seqs.log_decay[x.h];
+        if (warp == 8) {
+            // loads
+            const int b = p.seqs.cu == nullptr ? x.seq : 0;
+            for (int c = x.c0; c < x.c1 && on; ++c, next()) {
+                const int t = (int)x.start + (back ? x.n - (c + 1) * C : c * C);          // (whole chunks: the ragged one is the last segment's)
+                on = warp_wait(sh, &sh.empty[stage], full_par ^ 1u);
+                if (!on) break;
+                if (elect_one()) {
+                    const uint32_t at = ring + (uint32_t)stage * STAGE;
+                    mbar_expect_tx(&sh.full[stage], STAGE);
+#pragma unroll
+                    for (int r = 1; r < 3; ++r) {
+                        const int m = p.which[x.job][r], hh = p.flat[m] & 2 ? 0 : x.h, bb = p.flat[m] & 1 ? 0 : b;
+#pragma unroll
+                        for (int d = 0; d < (r == 2 ? DV : DK); d += 64)
+                            tma_load_4d(at + (r == 2 ? V : 0u) + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
+                    }
+                }
+                __syncwarp();
+            }
+        } else if (warp == 9) {
+            // products
+            const uint32_t iv = IDESC | (1u << 16) | ((uint32_t)(job.Dv >> 3) << 17);
+            for (int c = x.c0; c < x.c1 && on; ++c, next()) {
+                const int s = g & 1;
+                const uint32_t par = (uint32_t)(g >> 1) & 1u, at = ring + (uint32_t)stage * STAGE, d = tm + STATE_U + 128 * s, a = tm + STATE_K + 128 * s;
+                on = warp_wait(sh, &sh.full[stage], full_par);
+                if (on) on = warp_wait(sh, &sh.k_ready[s], par);
+                if (on && g >= 2) on = warp_wait(sh, &sh.u_free[s], par ^ 1u);
+                if (!on) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t kd = desc_mn(at, C * 128), vd = desc_mn(at + V, C * 128);
+                    constexpr uint64_t K16 = 2048 >> 4;
+                    if (three)
+#pragma unroll
+                        for (int k = 0; k < C / 16; ++k) umma_bf16(d, kd + k * K16, vd + k * K16, iv | (1u << 15), k > 0);
+#pragma unroll
+                    for (int k = 0; k < C / 16; ++k) umma_ts(d, a + 64 + 8 * k, vd + k * K16, iv, three || k > 0);
+#pragma unroll
+                    for (int k = 0; k < C / 16; ++k) umma_ts(d, a + 8 * k, vd + k * K16, iv, true);
+                    umma_commit(&sh.u_full[s]);
+                    umma_commit(&sh.empty[stage]);
+                }
+                __syncwarp();
+            }
+        } else if (warp < 4) {
+            // K
+            const uint32_t panel = ring + (uint32_t)((quad >> 1) * (C * 128) + (((lane >> 4) << 3) + (lane & 7)) * 128), piece = (uint32_t)(quad & 1) * 4;
+            const uint32_t shift[2] = {((piece + ((lane >> 3) & 1)) ^ (uint32_t)(lane & 7)) << 4, ((piece + 2 + ((lane >> 3) & 1)) ^ (uint32_t)(lane & 7)) << 4};
+            __syncwarp();
+            k_weights(sh.wk[quad], sh.wk1[quad], sh.wk2[quad], ld, job.sum_scale, C, back, lane);
+            __syncwarp();
+            for (int c = x.c0; c < x.c1 && on; ++c, next()) {
+                const int s = g & 1;
+                on = warp_wait(sh, &sh.full[stage], full_par);
+                if (on && g >= 2) on = warp_wait(sh, &sh.u_full[s], ((uint32_t)(g >> 1) & 1u) ^ 1u);
+                if (!on) break;
+                tc_fence_after();
+                if (quad * 32 < DK) {
+                    const uint32_t from = panel + (uint32_t)stage * STAGE, to = lanes + STATE_K + 128 * s;
+                    if (three) {
+                        uint32_t low[2][2][4];
+#pragma unroll 1
+                        for (int j = 0; j < C; j += 32) {
+                            k_pieces3<2>(from + (uint32_t)(j * 128), shift, to + j / 2, sh.wk[quad] + j, lane, low);
+                            k_low<2>(from + (uint32_t)(j * 128), shift, low);
+                        }
+                    } else k_pieces2(from, shift, to, sh.wk1[quad], sh.wk2[quad], lane, C);
+                    tmem_wait_st();
+                }
+                tmem_arrive(&sh.k_ready[s]);
+            }
+        } else if (warp < 8) {
+            // S
+            f2 S[DV / 2];
+#pragma unroll
+            for (int v = 0; v < DV / 2; ++v) S[v] = 0;
+            for (int c = x.c0; c < x.c1; ++c, next()) {
+                const int s = g & 1;
+                const LaStep step(ld, C - (c == 0 && back ? 1 : 0));
+                if (on) on = warp_wait(sh, &sh.u_full[s], (uint32_t)(g >> 1) & 1u);
+                if (!on) break;
+                tc_fence_after();
+                if (quad * 32 < DK) {
+                    const f2 w = pair(step.w, step.w), stay = pair(step.stay, step.stay);
+#pragma unroll
+                    for (int v = 0; v < DV; v += 16) {
+                        uint32_t U[16];
+                        tmem_ld16(lanes + STATE_U + 128 * s + v, U);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            f2 &y = S[v / 2 + e];
+                            y = fma2(stay, y, fma2(w, y, pair(__uint_as_float(U[2 * e]), __uint_as_float(U[2 * e + 1]))));
+                        }
+                    }
+                }
+                tmem_arrive(&sh.u_free[s]);
+            }
+            const int Dk = job.Dk, Dv = job.Dv;
+            if (row < Dk) {
+                const float f = on ? 1.0f : NAN;
+                float4 *const to = reinterpret_cast<float4 *>(p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * Dk * Dv + (size_t)row * Dv);
+#pragma unroll
+                for (int v = 0; v < DV; v += 4)
+                    if (v < Dv) to[v / 4] = make_float4(f * lo(S[v / 2]), f * hi(S[v / 2]), f * lo(S[v / 2 + 1]), f * hi(S[v / 2 + 1]));
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (sh.dead != 0)
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_dealloc(tm, 512);
     }
 }
 
-template <int DK, int DV, bool OUT>
-cudaError_t launch(const Params &p, int sms, cudaStream_t stream)
+// They become the states that the segments start from: C_0 = S0, C_{i+1} = lambda^seg C_i + own_i.  A thread per value; the loads do not wait for
+// the sums (eight segments' worth in flight).
+__global__ void la_carry_kernel(LaJobs jobs, LaSeqs seqs, int slots, int per, int seg, float *carry)
 {
-    auto kernel = la_tc_kernel<DK, DV, OUT>;
-    constexpr size_t smem = Layout<DK, DV, OUT>::SMEM;
+    const int job_i = blockIdx.z, h = blockIdx.x % seqs.H, seq = blockIdx.x / seqs.H;
+    const LaJob &job = jobs.job[job_i];
+    const int e = blockIdx.y * blockDim.x + threadIdx.x, size = job.Dk * job.Dv;
+    if (e >= size) return;
+    long long start;
+    const int n = la_sequence(seqs, seq, start);
+    const int slot = seqs.cu == nullptr ? seq * per : min(max(seqs.cu[seq], 0), (int)seqs.T) / seg + seq;
+    const int d = e / job.Dv, v = e % job.Dv, parts = (n + seg - 1) / seg;
+    float S = 0.0f;
+    if (job.s0 != nullptr) S = job.s0[((size_t)seq * seqs.H + h) * size + (job.turned ? (size_t)v * job.Dk + d : (size_t)e)];
+    const float ld = seqs.log_decay[h];
+    const LaStep step(ld, seg);
+    float *c = carry + (((size_t)job_i * slots + slot) * seqs.H + h) * size + e;
+    const size_t next = (size_t)seqs.H * size;
+    if (parts > 1) S = LaStep(ld, seg - (job.back ? 1 : 0))(S, *c);       // (the first segment starts from S0 itself)
+    c += next;
+    for (int i0 = 1; i0 < parts; i0 += 8, c += 8 * next) {
+        float own[8];                                        // the last segment's own state is not there, nor wanted
+#pragma unroll
+        for (int i = 0; i < 8; ++i) own[i] = i0 + i + 1 < parts ? c[i * next] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i0 + i < parts) {
+                c[i * next] = S;
+                S = step(S, own[i]);
+            }
+    }
+}
+
+template <int DK, int DV>
+cudaError_t launch(const Params &p, bool states, int sms, cudaStream_t stream)
+{
+    auto kernel = states ? la_state_kernel<DK, DV> : la_tc_kernel<DK, DV>;
+    const size_t smem = states ? 3 * C * (DK + DV) * 2 + 1024 : Layout<DK, DV>::SMEM;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)std::min<long long>(p.units, sms), TH, smem, stream>>>(p);
+    kernel<<<(unsigned)std::min(p.units, sms), states ? STATE_TH : TH, smem, stream>>>(p);
     return cudaGetLastError();
 }
-template <bool OUT>
-cudaError_t launch(const Params &p, int dk, int dv, int sms, cudaStream_t stream)
+cudaError_t launch(const Params &p, int dk, int dv, bool states, int sms, cudaStream_t stream)
 {
-    return dk <= 64 ? (dv <= 64 ? launch<64, 64, OUT>(p, sms, stream) : launch<64, 128, OUT>(p, sms, stream))
-                    : (dv <= 64 ? launch<128, 64, OUT>(p, sms, stream) : launch<128, 128, OUT>(p, sms, stream));
+    return dk <= 64 ? (dv <= 64 ? launch<64, 64>(p, states, sms, stream) : launch<64, 128>(p, states, sms, stream))
+                    : (dv <= 64 ? launch<128, 64>(p, states, sms, stream) : launch<128, 128>(p, states, sms, stream));
 }
 
 int sm_count()
@@ -652,19 +1008,20 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
     const long long n = s->cu_seqlens != nullptr ? s->N : s->B, heads = std::max(1ll, n * s->H * jobs), sms = sm_count();
     const long long steps = s->cu_seqlens != nullptr ? (n > 0 ? (s->T + n - 1) / n : 0) : s->T, chunks = (steps + C - 1) / C;
     long long best = std::max(1ll, (s->T + C - 1) / C), cost = (heads + sms - 1) / sms * chunks;
-    for (long long parts = 2; parts <= 64 && parts <= chunks; ++parts) {
-        const long long per = (chunks + parts - 1) / parts, c = (heads * parts + sms - 1) / sms * per * 8 / 5 + 6;
+    for (long long parts = 2; parts <= 64 && 4 * parts <= chunks; ++parts) {
+        const long long per = (chunks + parts - 1) / parts, c = (heads * parts + sms - 1) / sms * (per + 1) * 8 / 5 + 6;
         if (c < cost) { cost = c; best = per; }
     }
     LaPlan plan;
-    plan.seg = best * C;
+    plan.seg = (int)std::min(best * C, 1ll << 30);
     const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
-    plan.slots = (int)slots;
-    plan.bytes = slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
+    plan.fits = slots * s->H * jobs < (1ll << 31) && s->T < (1ll << 30);
+    plan.slots = plan.fits ? (int)slots : 0;
+    plan.bytes = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
     return plan;
 }
 
-bool la_tc_takes(const la_shape *s, const la_tensor *const *tensors, int count)
+bool la_tc_takes(const la_shape *s, int jobs, const la_tensor *const *tensors, int count)
 {
     if (s->type != LA_BF16 || s->Dk % 16 || s->Dv % 16 || s->T < 1) return false;
     for (int i = 0; i < count; ++i) {
@@ -674,7 +1031,7 @@ bool la_tc_takes(const la_shape *s, const la_tensor *const *tensors, int count)
             if (st % 8 != 0 || st < 0 || st >= (1ll << 38)) return false;
         if (t.token == 0 && s->T > 1) return false;
     }
-    return js_tensor_maps();
+    return la_tc_plan(s, jobs).fits && js_tensor_maps();
 }
 
 cudaError_t la_tc_run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const *inputs, int n_in, const int (*which)[3], void *workspace,
@@ -705,16 +1062,17 @@ cudaError_t la_tc_run(const la_shape *s, const LaJobs &jobs, int count, const la
     p.seqs = LaSeqs{n, s->H, s->T, s->cu_seqlens, s->log_decay};
     p.jobs = count;
     p.slots = plan.slots;
+    p.per = std::max(1, plan.slots / n);
     p.seg = plan.seg;
     p.carry = (float *)workspace;
-    p.units = (long long)plan.slots * s->H * count;
+    p.units = plan.slots * s->H * count;
     const int sms = sm_count();
     if (plan.slots > n) {
-        cudaError_t e = launch<false>(p, dk, dv, sms, stream);
+        cudaError_t e = launch(p, dk, dv, true, sms, stream);
         if (e != cudaSuccess) return e;
-        la_carry_kernel<<<dim3((unsigned)(n * s->H), (unsigned)((s->Dk * s->Dv + 255) / 256), (unsigned)count), 256, 0, stream>>>(p);
+        la_carry_kernel<<<dim3((unsigned)(n * s->H), (unsigned)((s->Dk * s->Dv + 255) / 256), (unsigned)count), 256, 0, stream>>>(jobs, p.seqs, p.slots, p.per, p.seg, p.carry);
         e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    return launch<true>(p, dk, dv, sms, stream);
+    return launch(p, dk, dv, false, sms, stream);
 }
