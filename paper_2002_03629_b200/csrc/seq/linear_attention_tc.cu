@@ -30,10 +30,10 @@ constexpr int TH = 448;                      // 4 + 8 + 2 warps: four to a sched
 constexpr uint32_t COL_SC = 0, COL_U = 128, COL_O = 256, COL_K = 384;      // scores and P; own sum; output; K's upper pieces
 
 struct Params {
-    CUtensorMap map[4];
+    CUtensorMap map[4], out[3];              // inputs, boxes of 64 values x C steps; a job's output, 64 x 32
     LaJob job[3];
     int which[3][3];                         // a job's q, k, v: number of the tensor map
-    int flat[4];                             // tensors whose batch (1) or head (2) stride is 0: coordinate 0
+    int flat[4], out_flat[3];                // tensors whose batch (1) or head (2) stride is 0, or that have only one: coordinate 0
     LaSeqs seqs;
     int jobs, slots, per;                    // slots: segments of all sequences; per: of one, where all are alike
     int seg;                                 // steps of a segment, a multiple of C
@@ -81,23 +81,28 @@ __device__ __forceinline__ bool get_unit(const Params &p, int u, Unit &x)
     return true;
 }
 
-// What the roles need to know of a chunk.  The loading warp works it out and hands it on through a ring, so that the code that finds
-// units (divisions, searches) is not in every role's loop.
-enum : int { FIRST = 1, LAST = 2, STATE = 4, LATE = 8, WEAK = 16, THREE = 32, BACK = 64, NONE = 128, END = 256 };
-struct alignas(16) Chunk {
-    int flags, rows, job;                    // FIRST, LAST of its unit; STATE: there is one before it; NONE: the unit has no steps
+// What the roles need to know of a unit.  The loading warp works it out and hands it on through a ring, so that the code that finds
+// units (divisions, searches) is not in every role.
+enum : int { BACK = 1, THREE = 2, WEAK = 4, INIT = 8, TURNED = 16, END = 32 };
+struct alignas(16) Work {
+    int flags;                               // THREE: K in three pieces; INIT: there is a state before the first chunk; TURNED: it lies transposed
+    int n, c0, c1;                           // steps of the sequence, chunks [c0, c1) of it
+    int job, h, b, start;                    // b: batch row; start: the sequence's first step there
     float ld, sum_scale, last;               // last: factor of the state that is handed out
-    __nv_bfloat16 *out;                      // first row
-    const float *from;                       // the unit's first state (NULL: zeros) and where its last one goes (NULL: nowhere)
+    const float *from;                       // the first state, and where the last one goes (NULL: nowhere)
     float *to;
-    int turned;
+    // steps of chunk c; is the state before it taken one step later than its first position? is there a state before it?
+    __device__ __forceinline__ int rows(int c) const { return min(C, n - c * C); }
+    __device__ __forceinline__ int late(int c) const { return c == 0 && (flags & BACK) ? 0 : 1; }
+    __device__ __forceinline__ bool state(int c) const { return c > c0 || (flags & INIT); }
+    __device__ __forceinline__ int step(int c) const { return start + (flags & BACK ? n - c * C - rows(c) : c * C); }      // its first row
 };
 constexpr int RING = 4, ROLE_WARPS = 13;
 
 struct Shared {
     uint64_t full[4], empty[4], told[RING], heard[RING];
     uint64_t sc_full, p_ready, k_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
-    Chunk chunk[RING];
+    Work work[RING];
     uint32_t tmem;
     int dead;
     // weights of the scores' columns; of K's rows, in fp32 and as two bf16 pieces, rows 2 i and 2 i + 1 in word i.  (A table is written by each
@@ -166,6 +171,11 @@ __device__ __forceinline__ void stsm4_t(uint32_t at, const uint32_t (&r)[4])
 __device__ __forceinline__ void tmem_st_16x8(uint32_t taddr, const uint32_t (&r)[4])
 {
     asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap *map, uint32_t src, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 // two fp32 values in a register pair, and operations on both
 typedef unsigned long long f2;
@@ -242,40 +252,32 @@ __device__ __forceinline__ void k_weights(float *wk, uint32_t *wk1, uint32_t *wk
         wk2[i] = narrow(add2(pair(w[0], w[1]), wide_negative(w1)));
     }
 }
-// 32 columns of K over 16 N steps, weighted and transposed, as three bf16 pieces: two into tensor memory (`to`, and 64 columns on), the third into
-// `low`, which k_low() puts where K was
-template <int N>
-__device__ __forceinline__ void k_pieces3(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const float *wk, int lane, uint32_t (&low)[N][2][4])
+// 32 columns of K, weighted and transposed, as three bf16 pieces: two into tensor memory (`to`, and 64 columns on), the third back to where K was
+__device__ __forceinline__ void k_pieces3(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const float *wk, int lane, int steps)
 {
     const f2 *w = reinterpret_cast<const f2 *>(wk) + (lane & 3), minus = pair(-1.0f, -1.0f);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const f2 ww[2] = {w[8 * j], w[8 * j + 4]};
-#pragma unroll
-        for (int g = 0; g < 2; ++g) ldsm4_t(from + (uint32_t)(j * 2048) + shift[g], low[j][g]);
+#pragma unroll 1
+    for (int j = 0; j < steps; j += 16, from += 2048, to += 8, w += 8) {
+        const f2 ww[2] = {w[0], w[4]};
+        uint32_t k[2][4];
+        ldsm4_t(from + shift[0], k[0]);
+        ldsm4_t(from + shift[1], k[1]);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             uint32_t h[4], m[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                f2 y = mul2(wide(low[j][g][e]), ww[e >> 1]);
+                f2 y = mul2(wide(k[g][e]), ww[e >> 1]);
                 h[e] = narrow(y);
                 y = fma2(wide(h[e]), minus, y);
                 m[e] = narrow(y);
-                low[j][g][e] = narrow(fma2(wide(m[e]), minus, y));
+                k[g][e] = narrow(fma2(wide(m[e]), minus, y));
             }
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 8 * j, h);
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64 + 8 * j, m);
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16), h);
+            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64, m);
+            stsm4_t(from + shift[g], k[g]);
         }
     }
-}
-template <int N>
-__device__ __forceinline__ void k_low(uint32_t from, const uint32_t (&shift)[2], const uint32_t (&low)[N][2][4])
-{
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) stsm4_t(from + (uint32_t)(j * 2048) + shift[g], low[j][g]);
     fence_proxy_async_smem();
 }
 // The same as two pieces, by bf16 arithmetic: k w1 = h + t exactly (8 by 8 bits), t + k w2 rounded once
@@ -303,18 +305,18 @@ __device__ __forceinline__ void k_pieces2(uint32_t from, const uint32_t (&shift)
     }
 }
 
-// a role's place in the ring of chunks
+// a role's place in the ring of units
 struct Place {
     int at = 0;
     uint32_t par = 0;
-    __device__ __forceinline__ bool next(Shared &sh, Chunk &c, bool on)
+    __device__ __forceinline__ bool next(Shared &sh, Work &w)
     {
-        if (!on || !warp_wait(sh, &sh.told[at], par)) return false;
-        c = sh.chunk[at];
+        if (!warp_wait(sh, &sh.told[at], par)) return false;
+        w = sh.work[at];
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.heard[at]);
         if (++at == RING) { at = 0; par ^= 1u; }
-        return (c.flags & END) == 0;
+        return (w.flags & END) == 0;
     }
 };
 
@@ -339,7 +341,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     const uint32_t s_smem = smem_u32(base), ring = s_smem + L::S_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
     if (tid == 0) {
-        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 5); }
         for (int i = 0; i < RING; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.heard[i], ROLE_WARPS); }
         mbar_init(&sh.sc_full, 1); mbar_init(&sh.qs_done, 1); mbar_init(&sh.u_full, 1); mbar_init(&sh.o_full, 1);
         mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.s_ready, 8);
@@ -352,110 +354,98 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     __syncthreads();
     tc_fence_after();
     const uint32_t tm = sh.tmem, lanes = tm + ((uint32_t)(quad * 32) << 16);
-    if (warp >= 12) {
-        if (warp == 12) {
-            // ---------------------------------------------------------------- loads
-            int stage = 0, slot = 0;
-            uint32_t par = 1, heard_par = 1;
-            bool on = true;
-            auto tell = [&](const Chunk &c) {
-                on = warp_wait(sh, &sh.heard[slot], heard_par);
-                if (!on) return;
-                if (lane == 0) {
-                    sh.chunk[slot] = c;
-                    mbar_arrive(&sh.told[slot]);
-                }
-                if (++slot == RING) { slot = 0; heard_par ^= 1u; }
-            };
-            Chunk k{};
-            for (int u = blockIdx.x; u < p.units && on; u += gridDim.x) {
-                Unit x;
-                if (!get_unit(p, u, x)) continue;
-                const LaJob &job = p.job[x.job];
-                const int b = p.seqs.cu == nullptr ? x.seq : 0, size = job.Dk * job.Dv;
-                const size_t state = ((size_t)x.seq * p.seqs.H + x.h) * size;
-                float *const carry = p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * size;
-                k.job = x.job;
-                k.ld = p.seqs.log_decay[x.h];
-                k.sum_scale = job.sum_scale;
-                k.last = job.back && x.n > 0 ? la_power(k.ld, 1) : 1.0f;
-                k.from = x.c0 > 0 ? carry : job.s0 != nullptr ? job.s0 + state : nullptr;
-                k.turned = x.c0 == 0 && job.turned;
-                const int same = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (k.ld >= -44.0f / MID ? WEAK : 0);
-                __nv_bfloat16 *const out = (__nv_bfloat16 *)job.o.data + b * job.o.batch + x.h * job.o.head;
-                float *const to = x.last && job.s1 != nullptr ? job.s1 + state : nullptr;
-                if (x.c0 == x.c1) {
-                    k.flags = same | FIRST | LAST | NONE;
-                    k.rows = 0;
-                    k.to = to;
-                    tell(k);
-                    continue;
-                }
-                for (int c = x.c0; c < x.c1 && on; ++c) {
-                    const bool first = c == x.c0, last = c + 1 == x.c1;
-                    k.rows = min(C, x.n - c * C);
-                    const int t = (int)x.start + (job.back ? x.n - c * C - k.rows : c * C);
-                    k.flags = same | (first ? FIRST : 0) | (last ? LAST : 0) | (!first || k.from != nullptr ? STATE : 0) | (c == 0 && job.back ? 0 : LATE);
-                    k.out = out + (long long)t * job.o.token;
-                    k.to = last ? to : nullptr;
-                    tell(k);
-                    if (on) on = warp_wait(sh, &sh.empty[stage], par);
-                    if (!on) break;
-                    if (elect_one()) {
-                        const uint32_t at = ring + (uint32_t)stage * L::STAGE;
-                        mbar_expect_tx(&sh.full[stage], L::STAGE);
-#pragma unroll
-                        for (int r = 0; r < 3; ++r) {
-                            const int m = p.which[x.job][r], hh = p.flat[m] & 2 ? 0 : x.h, bb = p.flat[m] & 1 ? 0 : b;
-                            const uint32_t to = at + (r == 0 ? L::Q : r == 1 ? L::K : L::V);
-#pragma unroll
-                            for (int d = 0; d < (r == 2 ? DV : DK); d += 64)
-                                tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
-                        }
-                    }
-                    __syncwarp();
-                    if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
-                }
+    if (warp == 12) {
+        // ---------------------------------------------------------------- loads
+        int stage = 0, slot = 0;
+        uint32_t par = 1, heard_par = 1;
+        bool on = true;
+        auto tell = [&](const Work &w) {
+            on = warp_wait(sh, &sh.heard[slot], heard_par);
+            if (!on) return;
+            if (lane == 0) {
+                sh.work[slot] = w;
+                mbar_arrive(&sh.told[slot]);
             }
-            k.flags = END;
-            if (on) tell(k);
-        } else {
-            // ---------------------------------------------------------------- products
-            int stage = 0;
-            uint32_t full_par = 0, par = 0, s_par = 0, o_par = 0;          // par: barriers that complete once a chunk
-            bool on = true, first = true;
-            const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0);            // (known to the compiler as the same in all lanes)
-            auto wait = [&](uint64_t *bar, uint32_t parity) {
-                if (on) on = warp_wait(sh, bar, parity);
-                tc_fence_after();
-            };
-            Place place;
-            Chunk ch;
-            while (place.next(sh, ch, on)) {
-                const int flags = __shfl_sync(0xffffffffu, ch.flags, 0), job = __shfl_sync(0xffffffffu, ch.job, 0);
-                if (flags & NONE) continue;
-                const bool state = flags & STATE;
-                const uint32_t ik = IDESC | ((uint32_t)(C >> 3) << 17), iv = IDESC | (1u << 16) | ((uint32_t)(p.job[job].Dv >> 3) << 17);
-                const int nk = p.job[job].Dk / 16;
+            __syncwarp();
+            if (++slot == RING) { slot = 0; heard_par ^= 1u; }
+        };
+        Work w{};
+#pragma unroll 1
+        for (int u = blockIdx.x; u <= p.units + (int)gridDim.x && on; u += gridDim.x) {
+            Unit x{};
+            const bool end = u >= p.units;
+            if (!end && !get_unit(p, u, x)) continue;
+            const LaJob &job = p.job[x.job];
+            const size_t size = (size_t)job.Dk * job.Dv, state = ((size_t)x.seq * p.seqs.H + x.h) * size;
+            w.n = x.n; w.c0 = x.c0; w.c1 = x.c1;
+            w.job = x.job; w.h = x.h; w.start = (int)x.start;
+            w.b = p.seqs.cu == nullptr ? x.seq : 0;
+            w.ld = p.seqs.log_decay[x.h];
+            w.sum_scale = job.sum_scale;
+            w.last = job.back && x.n > 0 ? la_power(w.ld, 1) : 1.0f;
+            w.from = x.c0 > 0 ? p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * size : job.s0 != nullptr ? job.s0 + state : nullptr;
+            w.to = x.last && job.s1 != nullptr ? job.s1 + state : nullptr;
+            w.flags = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (w.ld >= -44.0f / MID ? WEAK : 0) | (w.from != nullptr ? INIT : 0) |
+                      (x.c0 == 0 && job.turned ? TURNED : 0) | (end ? END : 0);
+            tell(w);
+            if (end) break;
+#pragma unroll 1
+            for (int c = w.c0; c < w.c1 && on; ++c) {
+                const int t = w.step(c);
+                on = warp_wait(sh, &sh.empty[stage], par);
+                if (!on) break;
+                if (elect_one()) {
+                    const uint32_t at = ring + (uint32_t)stage * L::STAGE;
+                    mbar_expect_tx(&sh.full[stage], L::STAGE);
+#pragma unroll
+                    for (int r = 0; r < 3; ++r) {
+                        const int m = p.which[w.job][r], hh = p.flat[m] & 2 ? 0 : w.h, bb = p.flat[m] & 1 ? 0 : w.b;
+                        const uint32_t to = at + (r == 0 ? L::Q : r == 1 ? L::K : L::V);
+#pragma unroll
+                        for (int d = 0; d < (r == 2 ? DV : DK); d += 64)
+                            tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
+                    }
+                }
+                __syncwarp();
+                if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
+            }
+        }
+    } else if (warp == 13) {
+        // ---------------------------------------------------------------- products
+        int stage = 0;
+        uint32_t full_par = 0, par = 0, s_par = 0, o_par = 0;              // par: barriers that complete once a chunk
+        bool on = true, first = true;
+        const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0);                // (known to the compiler as the same in all lanes)
+        auto wait = [&](uint64_t *bar, uint32_t parity) {
+            if (on) on = warp_wait(sh, bar, parity);
+            tc_fence_after();
+        };
+        Place place;
+        Work w;
+        while (on && place.next(sh, w)) {
+            const int flags = __shfl_sync(0xffffffffu, w.flags, 0), job = __shfl_sync(0xffffffffu, w.job, 0);
+            const int c1 = __shfl_sync(0xffffffffu, w.c1, 0), c0 = __shfl_sync(0xffffffffu, w.c0, 0);
+            const uint32_t ik = IDESC | ((uint32_t)(C >> 3) << 17), iv = IDESC | (1u << 16) | ((uint32_t)(p.job[job].Dv >> 3) << 17);
+            const int nk = p.job[job].Dk / 16;
+            constexpr uint64_t K16 = 2048 >> 4, PANEL = C * 128 >> 4;        // sixteen rows of an operand with N (or M) together; a panel of 64 values
+#pragma unroll 1
+            for (int c = c0; c < c1 && on; ++c) {
                 const uint32_t at = ring + (uint32_t)stage * L::STAGE;
-                const uint64_t vd = desc_mn(at + L::V, C * 128);
-                constexpr uint64_t K16 = 2048 >> 4;                                // sixteen rows of an operand with N (or M) together
-                // columns of tensor memory by K's pieces (or P) times V
+                const uint64_t vd = desc_mn(at + L::V, C * 128), qd = smem_desc_sw128(at + L::Q);
+                const bool state = c > c0 || (flags & INIT);
+                // columns of tensor memory by K's pieces (or P) times V.  (Rolled: the loops of all roles share one instruction cache.)
                 auto times_v = [&](uint32_t d, uint32_t a, bool add) {
-#pragma unroll
+#pragma unroll 2
                     for (int k = 0; k < C / 16; ++k) umma_ts(tmu + d, tmu + a + 8 * k, vd + k * K16, iv, add || k > 0);
-                };
-                // Q (its rows' values together) times the operand whose descriptor of step k is b(k)
-                auto q_times = [&](uint32_t d, uint32_t idesc, auto b) {
-                    const uint64_t qd = smem_desc_sw128(at + L::Q);
-#pragma unroll
-                    for (int k = 0; k < DK / 16; ++k)
-                        if (k < nk) umma_bf16(tmu + d, qd + (uint64_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2), b(k), idesc, k > 0);
                 };
                 wait(&sh.full[stage], full_par);
                 if (on && elect_one()) {
                     const uint64_t kd = smem_desc_sw128(at + L::K);
-                    q_times(COL_SC, ik, [&](int k) { return kd + (uint64_t)((k >> 2) * (C * 128 >> 4) + (k & 3) * 2); });
+#pragma unroll 2
+                    for (int k = 0; k < nk; ++k) {
+                        const uint64_t o = (uint64_t)(k >> 2) * PANEL + (uint64_t)(k & 3) * 2;
+                        umma_bf16(tmu + COL_SC, qd + o, kd + o, ik, k > 0);
+                    }
                     umma_commit(&sh.sc_full);
                 }
                 __syncwarp();
@@ -465,7 +455,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     // the small pieces first, while the sum is small: it is rounded towards zero at every step
                     if (flags & THREE) {
                         const uint64_t kd = desc_mn(at + L::K, C * 128);
-#pragma unroll
+#pragma unroll 2
                         for (int k = 0; k < C / 16; ++k) umma_bf16(tmu + COL_U, kd + k * K16, vd + k * K16, iv | (1u << 15), k > 0);
                     }
                     times_v(COL_U, COL_K + 64, flags & THREE);
@@ -479,8 +469,9 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     s_par ^= 1u;
                     if (on && elect_one()) {
                         const uint64_t sd = desc_mn(s_smem, DK * 128);
-                        q_times(COL_O, iv, [&](int k) { return sd + k * K16; });
-                        umma_commit(&sh.qs_done);
+#pragma unroll 2
+                        for (int k = 0; k < nk; ++k) umma_bf16(tmu + COL_O, qd + (uint64_t)(k >> 2) * PANEL + (uint64_t)(k & 3) * 2, sd + k * K16, iv, k > 0);
+                        if (!(flags & WEAK)) umma_commit(&sh.qs_done);
                     }
                     __syncwarp();
                 }
@@ -492,9 +483,8 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                 if (on && elect_one()) {
                     times_v(COL_O, COL_SC, state);
                     umma_commit(&sh.o_full);
+                    umma_commit(&sh.empty[stage]);
                 }
-                __syncwarp();
-                if (on && elect_one()) umma_commit(&sh.empty[stage]);
                 __syncwarp();
                 if (++stage == L::STAGES) { stage = 0; full_par ^= 1u; }
                 par ^= 1u;
@@ -502,147 +492,166 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             }
         }
     } else if (warp < 4) {
-        // ------------------------------------------------------------- P, and O of the chunk before
+        // ------------------------------------------------------------- O of the chunk before, and P
         uint32_t par = 0, qs_par = 0;
-        bool on = true;
-        // a chunk whose sum is still to go out
-        __nv_bfloat16 *out = nullptr;
-        float out_f = 0.0f;
-        int out_rows = 0, out_dv = 0;
-        bool due = false;
-        auto put_out = [&]() {
-            if (on) on = warp_wait(sh, &sh.o_full, par ^ 1u);
-            tc_fence_after();
-            const f2 ff = pair(out_f, out_f);
-            const bool in = row < out_rows;
+        bool on = true, more = true, due = false;
+        Place place;
+        Work w{};
+        int c = 0, out_stage = 0, had = -1;                                        // had: rows (and more) that the table is for
+        // the sum that is still to go out: its steps, factor, place
+        int out_rows = 0, out_job = 0, out_t = 0, out_h = 0, out_b = 0;
+        float out_f = 0.0f, full_f = 0.0f;
+        for (;;) {
+            while (more && c == w.c1) {
+                more = place.next(sh, w);
+                c = w.c0;
+                had = -1;
+                if (more) full_f = p.job[w.job].out_scale * (w.flags & WEAK ? power_of(w.ld, (w.flags & BACK ? C - 1 - row : row) + 1 - MID) : 1.0f);
+            }
+            bool stored = false;
+            if (due) {
+                // By way of shared memory, where the chunk's Q was, and a tensor store of the warp's 32 rows; the sequence's last rows by plain
+                // stores.  (Plain stores of all rows, 16 bytes to each of 32 rows at a time, kept the load-store unit busy for 2000 cycles a chunk.)
+                const LaJob &job = p.job[out_job];
+                const int Dv = job.Dv;
+                const bool in = row < out_rows, whole = out_rows >= quad * 32 + 32;
+                if (on) on = warp_wait(sh, &sh.o_full, par ^ 1u);
+                tc_fence_after();
+                stored = whole && on;
+                const f2 ff = pair(out_f, out_f);
+                const uint32_t box = ring + (uint32_t)out_stage * L::STAGE + L::Q + (uint32_t)(quad * 32 * 128);
+                __nv_bfloat16 *const to = (__nv_bfloat16 *)job.o.data + out_b * job.o.batch + out_h * job.o.head + (long long)(out_t + row) * job.o.token;
 #pragma unroll 1
-            for (int v = 0; v < out_dv; v += 64) {                                 // (columns beyond Dv hold something or other)
-                uint32_t r[32], q[32];
-                tmem_ld32_issue(lanes + COL_O + v, r);
-                tmem_ld32_issue(lanes + COL_O + v + 32, q);
-                tmem_wait_ld();
-                if (on && v + 64 >= out_dv) tmem_arrive(&sh.o_free);               // (before the last stores: the next sum may come)
+                for (int v = 0; v < Dv; v += 32) {                                 // (columns beyond Dv hold something or other)
+                    uint32_t r[32];
+                    tmem_ld32_issue(lanes + COL_O + v, r);
+                    tmem_wait_ld();
+                    if (on && v + 32 >= Dv) tmem_arrive(&sh.o_free);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    r[e] = narrow(mul2(pair(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), ff));
-                    q[e] = narrow(mul2(pair(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1])), ff));
+                    for (int e = 0; e < 16; ++e) r[e] = narrow(mul2(pair(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), ff));
+                    if (stored) {
+                        const uint32_t at = box + (uint32_t)((v >> 6) * (C * 128) + lane * 128);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sts128(at + ((uint32_t)((((v & 63) >> 3) + e) ^ (lane & 7)) << 4), r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
+                    } else if (in) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (v + 8 * e < Dv) {
+                                const uint4 y = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]), nan = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+                                *reinterpret_cast<uint4 *>(to + v + 8 * e) = on ? y : nan;       // (a wait gave up: NaN)
+                            }
+                    }
                 }
-                if (!on)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = q[e] = 0x7fff7fffu;        // a wait gave up: NaN
-                if (in) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (v + 8 * e < out_dv) *reinterpret_cast<uint4 *>(out + v + 8 * e) = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (v + 32 + 8 * e < out_dv) *reinterpret_cast<uint4 *>(out + v + 32 + 8 * e) = make_uint4(q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]);
+                if (stored) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        const int m = p.out_flat[out_job], hh = m & 2 ? 0 : out_h, bb = m & 1 ? 0 : out_b;
+#pragma unroll 1
+                        for (int v = 0; v < Dv; v += 64) tma_store_4d(&p.out[out_job], box + (uint32_t)((v >> 6) * (C * 128)), v, out_t + quad * 32, hh, bb);
+                        bulk_commit();
+                    }
                 }
             }
-        };
-        Place place;
-        Chunk ch;
-        int had = -1;                                                              // rows (and more) that the table is for
-        while (place.next(sh, ch, true)) {
-            if (ch.flags & NONE) continue;
-            const bool back = ch.flags & BACK, weak = ch.flags & WEAK;
-            const int rows = ch.rows, late = ch.flags & LATE ? 1 : 0;
-            if (due) put_out();
-            if (on) on = warp_wait(sh, &sh.sc_full, par);
-            if (on) {
-                tc_fence_after();
-                if ((ch.flags & FIRST) || had != 2 * rows + late) {
-                    had = 2 * rows + late;
-                    if (weak) {
+            const bool have = c < w.c1 && more;
+            if (have) {
+                const bool back = w.flags & BACK, weak = w.flags & WEAK, state = w.state(c);
+                const int rows = w.rows(c), late = w.late(c);
+                if (on) on = warp_wait(sh, &sh.sc_full, par);
+                if (on) {
+                    tc_fence_after();
+                    if (had != 2 * rows + late) {
+                        had = 2 * rows + late;
+                        if (weak) {
 #pragma unroll 1
-                        for (int j = lane; j < C; j += 32) sh.wp[j] = ch.sum_scale * power_of(ch.ld, MID - (back ? rows - 1 - j : j) - late);
-                    } else sh.wp[lane] = ch.sum_scale * la_power(ch.ld, back ? lane : 31 - lane);
-                    __syncwarp();
-                }
-                // Columns of block b that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
-                auto kept = [&](int b) -> uint32_t {
-                    const uint32_t own = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-                    const int there = rows - 32 * b;
-                    return (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) & (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
-                };
-                const int b0 = back ? quad : 0, b1 = back ? 4 : quad + 1;          // blocks with anything in them
-                if (weak) {
-#pragma unroll 1
-                    for (int b = 0; b < 4; b += 2) {                               // (two blocks' scores on their way at a time)
-                        uint32_t s[32], t[32], w[16];
-                        tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
-                        tmem_ld32_issue(lanes + COL_SC + 32 * b + 32, t);
-                        tmem_wait_ld();
-                        p_pack(s, w, sh.wp + 32 * b, kept(b));
-                        tmem_st16(lanes + COL_SC + 16 * b, w);
-                        p_pack(t, w, sh.wp + 32 * b + 32, kept(b + 1));
-                        tmem_st16(lanes + COL_SC + 16 * b + 16, w);
+                            for (int j = lane; j < C; j += 32) sh.wp[j] = w.sum_scale * power_of(w.ld, MID - (back ? rows - 1 - j : j) - late);
+                        } else sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
+                        __syncwarp();
                     }
-                } else {
 #pragma unroll 1
                     for (int b = 0; b < 4; ++b) {
-                        uint32_t s[32], w[16];
-                        tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
-                        tmem_wait_ld();
-                        if (b != quad) {
-                            // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
-                            const float f = b >= b0 && b < b1 ? la_power(ch.ld, back ? 32 * b - row : row - 32 * b - 31) : 0.0f;
+                        // Columns of the block that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
+                        const uint32_t own = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                        const int there = rows - 32 * b;
+                        const uint32_t keep = (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) &
+                                              (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
+                        uint32_t words[16];
+                        if (back ? b < quad : b > quad) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
-                            p_pack(s, w, sh.wp, kept(b));
+                            for (int e = 0; e < 16; ++e) words[e] = 0u;
                         } else {
-                            // the row's own block: the power of the distance
-                            const uint32_t keep = kept(b);
+                            uint32_t s[32];
+                            tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
+                            tmem_wait_ld();
+                            if (weak) p_pack(s, words, sh.wp + 32 * b, keep);
+                            else if (b != quad) {
+                                // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
+                                const float f = la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const int far = max(back ? e - lane : lane - e, 0);
-                                s[e] = keep >> e & 1u ? __float_as_uint(__uint_as_float(s[e]) * sh.wp[back ? far : 31 - far]) : 0u;
+                                for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
+                                p_pack(s, words, sh.wp, keep);
+                            } else {
+                                // the row's own block: the power of the distance
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    const int far = max(back ? e - lane : lane - e, 0);
+                                    s[e] = keep >> e & 1u ? __float_as_uint(__uint_as_float(s[e]) * sh.wp[back ? far : 31 - far]) : 0u;
+                                }
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) words[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
                             }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
                         }
-                        tmem_st16(lanes + COL_SC + 16 * b, w);
-                    }
-                }
-                tmem_wait_st();
-                tmem_arrive(&sh.p_ready);
-            }
-            const LaJob &job = p.job[ch.job];
-            const int pos = (back ? rows - 1 - row : row) + late;
-            const bool in = row < rows;
-            if (ch.flags & STATE) {
-                // (a barrier is waited for in every one of its phases: one that is two phases behind looks as if it had completed)
-                if (on) on = warp_wait(sh, &sh.qs_done, qs_par);
-                qs_par ^= 1u;
-                if (on && !weak) {
-                    const float g = in ? la_power(ch.ld, pos) : 0.0f;
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int v = 0; v < job.Dv; v += 16) {
-                        uint32_t r[16];
-                        tmem_ld16(lanes + COL_O + v, r);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
-                        tmem_st16(lanes + COL_O + v, r);
+                        tmem_st16(lanes + COL_SC + 16 * b, words);
                     }
                     tmem_wait_st();
-                    tmem_arrive(&sh.o_scaled);
+                    tmem_arrive(&sh.p_ready);
+                }
+                if (state && !weak) {
+                    if (on) on = warp_wait(sh, &sh.qs_done, qs_par);
+                    qs_par ^= 1u;
+                    if (on) {
+                        const float g = row < rows ? la_power(w.ld, (back ? rows - 1 - row : row) + late) : 0.0f;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int v = 0; v < p.job[w.job].Dv; v += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(lanes + COL_O + v, r);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
+                            tmem_st16(lanes + COL_O + v, r);
+                        }
+                        tmem_wait_st();
+                        tmem_arrive(&sh.o_scaled);
+                    }
                 }
             }
-            out = ch.out + (long long)row * job.o.token;
-            out_f = job.out_scale * (!weak ? 1.0f : in ? power_of(ch.ld, pos - MID) : 0.0f);
-            out_rows = rows;
-            out_dv = job.Dv;
+            if (due) {
+                if (lane == 0) {                                                   // the stage may be loaded again when the store has read it
+                    if (stored) bulk_wait_read();
+                    mbar_arrive(&sh.empty[out_stage]);
+                }
+                if (++out_stage == L::STAGES) out_stage = 0;
+            }
+            if (!have) break;
+            out_rows = w.rows(c);
+            out_job = w.job;
+            out_t = w.step(c);
+            out_h = w.h;
+            out_b = w.b;
+            out_f = full_f;
+            if ((w.flags & WEAK) && (out_rows != C || !w.late(c)))
+                out_f = row < out_rows ? p.job[w.job].out_scale * power_of(w.ld, (w.flags & BACK ? out_rows - 1 - row : row) + w.late(c) - MID) : 0.0f;
             due = true;
             par ^= 1u;
+            ++c;
         }
-        if (due) put_out();
+        if (lane == 0) bulk_wait_all();
     } else {
         // ------------------------------------------------------------- K and S
         int stage = 0;
-        uint32_t full_par = 0, par = 0, qs_par = 1;
-        bool on = true, wrote = false;
+        uint32_t full_par = 0, par = 0;
+        bool on = true;
         const int half = (warp - 4) >> 2;                                          // of a chunk's steps and of the state's columns
         constexpr int HV = DV / 2, HC = C / 2;
         const bool mine = row < DK;
@@ -656,90 +665,87 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
         const uint32_t s_row = s_smem + (uint32_t)((v0 >> 6) * (DK * 128) + row * 128), s_turn = (uint32_t)(row & 7) << 4;
         f2 S[HV / 2];
         Place place;
-        Chunk ch;
-        int had = 0;                                                               // rows that the tables are for
-        while (place.next(sh, ch, true)) {
-            const int Dk = p.job[ch.job].Dk, Dv = p.job[ch.job].Dv, rows = ch.rows;
+        Work w;
+        while (place.next(sh, w)) {
+            const int Dk = p.job[w.job].Dk, Dv = p.job[w.job].Dv;
             const bool have = mine && row < Dk;
-            if (ch.flags & FIRST) {
+            const LaStep whole(w.ld, C);
+            const float mid = w.flags & WEAK ? power_of(w.ld, MID) : 1.0f;
+            int had = 0;                                                           // rows that the tables are for
 #pragma unroll
-                for (int v = 0; v < HV / 2; ++v) S[v] = 0;
-                if (ch.from != nullptr && have) {
-                    if (ch.turned) {
-                        const float *r = ch.from + row + v0 * Dk;
+            for (int v = 0; v < HV / 2; ++v) S[v] = 0;
+            if (w.from != nullptr && have) {
+                if (w.flags & TURNED) {
+                    const float *r = w.from + row + v0 * Dk;
 #pragma unroll
-                        for (int v = 0; v < HV; v += 2)
-                            if (v0 + v < Dv) S[v / 2] = pair(r[v * Dk], r[(v + 1) * Dk]);
-                    } else {
-                        const float4 *r = reinterpret_cast<const float4 *>(ch.from + row * Dv + v0);
+                    for (int v = 0; v < HV; v += 2)
+                        if (v0 + v < Dv) S[v / 2] = pair(r[v * Dk], r[(v + 1) * Dk]);
+                } else {
+                    const float4 *r = reinterpret_cast<const float4 *>(w.from + row * Dv + v0);
 #pragma unroll
-                        for (int v = 0; v < HV; v += 4)
-                            if (v0 + v < Dv) {
-                                const float4 y = r[v / 4];
-                                S[v / 2] = pair(y.x, y.y);
-                                S[v / 2 + 1] = pair(y.z, y.w);
-                            }
-                    }
+                    for (int v = 0; v < HV; v += 4)
+                        if (v0 + v < Dv) {
+                            const float4 y = r[v / 4];
+                            S[v / 2] = pair(y.x, y.y);
+                            S[v / 2 + 1] = pair(y.z, y.w);
+                        }
                 }
             }
-            if (!(ch.flags & NONE)) {
+#pragma unroll 1
+            for (int c = w.c0; c < w.c1; ++c) {
+                const int rows = w.rows(c);
                 if (on) on = warp_wait(sh, &sh.full[stage], full_par);
-                if (on) {
-                    tc_fence_after();
-                    if ((ch.flags & FIRST) || rows != had) {                       // (this warp has seen the chunk before's products complete)
-                        had = rows;
-                        k_weights(sh.wk, sh.wk1, sh.wk2, ch.ld, ch.sum_scale, rows, ch.flags & BACK, lane);
-                        __syncwarp();
-                    }
-                    const uint32_t at = ring + (uint32_t)stage * L::STAGE, panel = panel0 + (uint32_t)stage * L::STAGE;
-                    if (rows < C) {                                                // steps behind the sequence's end: zeros, in V and in K
-                        if (half == 0 && row >= rows)
-#pragma unroll 1
-                            for (int d = 0; d < DV / 8; ++d) sts128(at + L::V + (uint32_t)((d >> 3) * (C * 128) + row * 128 + (d & 7) * 16), 0, 0, 0, 0);
-                        if (quad * 32 < DK)
-#pragma unroll 1
-                            for (int j = max(rows, half * HC) + (lane >> 2); j < (half + 1) * HC; j += 8)
-                                sts128(panel + (uint32_t)(j * 128) + (((piece + (uint32_t)(lane & 3)) ^ (uint32_t)(j & 7)) << 4), 0, 0, 0, 0);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                    }
-                    uint32_t low[HC / 16][2][4];
-                    if (quad * 32 < DK) {
-                        if (ch.flags & THREE) k_pieces3<HC / 16>(panel + from, shift, k_to, sh.wk + half * HC, lane, low);
-                        else k_pieces2(panel + from, shift, k_to, sh.wk1 + half * HC / 2, sh.wk2 + half * HC / 2, lane, HC);
-                        tmem_wait_st();
-                    }
-                    on = warp_wait(sh, &sh.sc_full, par);                          // K as it is has met Q: the third piece takes its place
-                    if (on && (ch.flags & THREE) && quad * 32 < DK) k_low<HC / 16>(panel + from, shift, low);
-                    if (on) tmem_arrive(&sh.k_ready);
+                // (every phase of a barrier is waited for: one that is two phases behind looks as if it had completed)
+                if (on) on = warp_wait(sh, &sh.sc_full, par);                      // K as it is has met Q: the third piece takes its place
+                if (!on) break;
+                tc_fence_after();
+                if (rows != had) {                                                 // (this warp has seen the chunk before's products complete)
+                    had = rows;
+                    k_weights(sh.wk, sh.wk1, sh.wk2, w.ld, w.sum_scale, rows, w.flags & BACK, lane);
+                    __syncwarp();
                 }
-                if (ch.flags & STATE) {
-                    // the state before the chunk to shared memory, in bf16, for Q S
-                    if (on && wrote) on = warp_wait(sh, &sh.qs_done, qs_par);      // the product with the one before is done
-                    wrote = true;
-                    qs_par ^= 1u;
-                    const float mid = ch.flags & WEAK ? power_of(ch.ld, MID) : 1.0f;
+                const uint32_t at = ring + (uint32_t)stage * L::STAGE, panel = panel0 + (uint32_t)stage * L::STAGE;
+                if (rows < C) {                                                    // steps behind the sequence's end: zeros, in V and in K
+                    if (half == 0 && row >= rows)
+#pragma unroll 1
+                        for (int d = 0; d < DV / 8; ++d) sts128(at + L::V + (uint32_t)((d >> 3) * (C * 128) + row * 128 + (d & 7) * 16), 0, 0, 0, 0);
+                    if (quad * 32 < DK)
+#pragma unroll 1
+                        for (int j = max(rows, half * HC) + (lane >> 2); j < (half + 1) * HC; j += 8)
+                            sts128(panel + (uint32_t)(j * 128) + (((piece + (uint32_t)(lane & 3)) ^ (uint32_t)(j & 7)) << 4), 0, 0, 0, 0);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                if (quad * 32 < DK) {
+                    if (w.flags & THREE) k_pieces3(panel + from, shift, k_to, sh.wk + half * HC, lane, HC);
+                    else k_pieces2(panel + from, shift, k_to, sh.wk1 + half * HC / 2, sh.wk2 + half * HC / 2, lane, HC);
+                    tmem_wait_st();
+                }
+                tmem_arrive(&sh.k_ready);
+                if (w.state(c)) {
+                    // the state before the chunk to shared memory, in bf16, for Q S (whose last product has met the one before it: sc_full came after)
                     if (mine) {
                         const f2 mm = pair(mid, mid);
 #pragma unroll
                         for (int v = 0; v < HV; v += 8) {
-                            uint32_t w[4];
+                            uint32_t r[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) w[e] = narrow(mul2(S[v / 2 + e], mm));
-                            sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), w[0], w[1], w[2], w[3]);
+                            for (int e = 0; e < 4; ++e) r[e] = narrow(mul2(S[v / 2 + e], mm));
+                            sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), r[0], r[1], r[2], r[3]);
                         }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.s_ready);
                 }
-                const LaStep step(ch.ld, rows - 1 + (ch.flags & LATE ? 1 : 0));
-                if (on) on = warp_wait(sh, &sh.u_full, par);
+                on = warp_wait(sh, &sh.u_full, par);
                 par ^= 1u;
                 if (++stage == L::STAGES) { stage = 0; full_par ^= 1u; }
+                if (!on) break;
                 tc_fence_after();
-                if (mine && on) {
-                    const f2 w = pair(step.w, step.w), stay = pair(step.stay, step.stay);
+                if (mine) {
+                    const LaStep step = rows == C && w.late(c) ? whole : LaStep(w.ld, rows - 1 + w.late(c));
+                    const f2 a = pair(step.w, step.w), stay = pair(step.stay, step.stay);
 #pragma unroll
                     for (int v = 0; v < HV; v += 32) {
                         uint32_t U[32];
@@ -748,15 +754,15 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             f2 &y = S[v / 2 + e];
-                            y = fma2(stay, y, fma2(w, y, pair(__uint_as_float(U[2 * e]), __uint_as_float(U[2 * e + 1]))));
+                            y = fma2(stay, y, fma2(a, y, pair(__uint_as_float(U[2 * e]), __uint_as_float(U[2 * e + 1]))));
                         }
                     }
                 }
-                if (on) tmem_arrive(&sh.u_free);
+                tmem_arrive(&sh.u_free);
             }
-            if ((ch.flags & LAST) && ch.to != nullptr && have) {
-                const float f = on ? ch.last : NAN;
-                float4 *const to = reinterpret_cast<float4 *>(ch.to + row * Dv + v0);
+            if (w.to != nullptr && have) {
+                const float f = on ? w.last : NAN;
+                float4 *const to = reinterpret_cast<float4 *>(w.to + row * Dv + v0);
 #pragma unroll
                 for (int v = 0; v < HV; v += 4)
                     if (v0 + v < Dv) to[v / 4] = make_float4(f * lo(S[v / 2]), f * hi(S[v / 2]), f * lo(S[v / 2 + 1]), f * hi(S[v / 2 + 1]));
@@ -768,6 +774,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     __syncthreads();
     // After a wait that gave up: what is on its way (copies, MMAs), microseconds' worth, ends before shared and tensor memory are given back.
     if (sh.dead != 0)
+#pragma unroll 1
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     if (warp == 12) {
         tc_fence_after();
@@ -883,14 +890,8 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
                 tc_fence_after();
                 if (quad * 32 < DK) {
                     const uint32_t from = panel + (uint32_t)stage * STAGE, to = lanes + STATE_K + 128 * s;
-                    if (three) {
-                        uint32_t low[2][2][4];
-#pragma unroll 1
-                        for (int j = 0; j < C; j += 32) {
-                            k_pieces3<2>(from + (uint32_t)(j * 128), shift, to + j / 2, sh.wk[quad] + j, lane, low);
-                            k_low<2>(from + (uint32_t)(j * 128), shift, low);
-                        }
-                    } else k_pieces2(from, shift, to, sh.wk1[quad], sh.wk2[quad], lane, C);
+                    if (three) k_pieces3(from, shift, to, sh.wk[quad], lane, C);
+                    else k_pieces2(from, shift, to, sh.wk1[quad], sh.wk2[quad], lane, C);
                     tmem_wait_st();
                 }
                 tmem_arrive(&sh.k_ready[s]);
@@ -936,6 +937,7 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
     tc_fence_before();
     __syncthreads();
     if (sh.dead != 0)
+#pragma unroll 1
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     if (warp == 8) {
         tc_fence_after();
@@ -1015,7 +1017,7 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
     LaPlan plan;
     plan.seg = (int)std::min(best * C, 1ll << 30);
     const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
-    plan.fits = slots * s->H * jobs < (1ll << 31) && s->T < (1ll << 30);
+    plan.fits = slots * s->H * jobs < (1ll << 30) && s->T < (1ll << 30);
     plan.slots = plan.fits ? (int)slots : 0;
     plan.bytes = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
     return plan;
@@ -1040,21 +1042,26 @@ cudaError_t la_tc_run(const la_shape *s, const LaJobs &jobs, int count, const la
     const LaPlan plan = la_tc_plan(s, count);
     const int n = s->cu_seqlens != nullptr ? s->N : s->B;
     Params p{};
+    // boxes of 64 values x `steps`
+    auto encode = [&](CUtensorMap &map, int &flat, const la_tensor &t, int width, int steps) {
+        flat = (t.batch == 0 || s->B == 1 ? 1 : 0) | (t.head == 0 || s->H == 1 ? 2 : 0);
+        const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)s->T, (cuuint64_t)(flat & 2 ? 1 : s->H), (cuuint64_t)(flat & 1 ? 1 : s->B)};
+        const cuuint64_t strides[3] = {(cuuint64_t)std::max(t.token, 8ll) * 2, (cuuint64_t)(flat & 2 ? 8 : t.head) * 2, (cuuint64_t)(flat & 1 ? 8 : t.batch) * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)steps, 1, 1};
+        return js_encode_map(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, t.data, 4, dims, strides, box);
+    };
     for (int i = 0; i < n_in; ++i) {
         const la_tensor &t = *inputs[i];
         int width = 0;                       // a head's values: by the first role that the tensor has
         for (int j = 0; j < count; ++j)
             for (int r = 0; r < 3; ++r)
                 if (which[j][r] == i) width = r == 2 ? jobs.job[j].Dv : jobs.job[j].Dk;
-        p.flat[i] = (t.batch == 0 || s->B == 1 ? 1 : 0) | (t.head == 0 || s->H == 1 ? 2 : 0);
-        const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)s->T, (cuuint64_t)(p.flat[i] & 2 ? 1 : s->H), (cuuint64_t)(p.flat[i] & 1 ? 1 : s->B)};
-        const cuuint64_t strides[3] = {(cuuint64_t)std::max(t.token, 8ll) * 2, (cuuint64_t)(p.flat[i] & 2 ? 8 : t.head) * 2, (cuuint64_t)(p.flat[i] & 1 ? 8 : t.batch) * 2};
-        const cuuint32_t box[4] = {64, C, 1, 1};
-        if (!js_encode_map(&p.map[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, t.data, 4, dims, strides, box)) return cudaErrorInvalidValue;
+        if (!encode(p.map[i], p.flat[i], t, width, C)) return cudaErrorInvalidValue;
     }
     int dk = 0, dv = 0;
     for (int j = 0; j < count; ++j) {
         p.job[j] = jobs.job[j];
+        if (!encode(p.out[j], p.out_flat[j], p.job[j].o, p.job[j].Dv, 32)) return cudaErrorInvalidValue;
         dk = std::max(dk, p.job[j].Dk);
         dv = std::max(dv, p.job[j].Dv);
         for (int r = 0; r < 3; ++r) p.which[j][r] = which[j][r];
