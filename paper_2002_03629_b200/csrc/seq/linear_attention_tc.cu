@@ -81,11 +81,19 @@ __device__ __forceinline__ bool get_unit(const Params &p, int u, Unit &x)
     return true;
 }
 
+// Where the last state is asked for, a chunk's sum reaches it with the weight lambda^(steps behind the chunk).  Two pieces of K leave the sum off by
+// 3e-6; under e^-6 that is lost in the state's own roundings, and the third piece is left out.
+__device__ __forceinline__ bool three_pieces(float log_decay, int n, int c)
+{
+    const int behind = n - (c + 1) * C;
+    return behind <= 0 || (float)behind * log_decay > -6.0f;
+}
+
 // What the roles need to know of a unit.  The loading warp works it out and hands it on through a ring, so that the code that finds
 // units (divisions, searches) is not in every role.
 enum : int { BACK = 1, THREE = 2, WEAK = 4, INIT = 8, TURNED = 16, END = 32 };
 struct alignas(16) Work {
-    int flags;                               // THREE: K in three pieces; INIT: there is a state before the first chunk; TURNED: it lies transposed
+    int flags;                               // THREE: the last state is asked for; INIT: there is a state before the first chunk; TURNED: it lies transposed
     int n, c0, c1;                           // steps of the sequence, chunks [c0, c1) of it
     int job, h, b, start;                    // b: batch row; start: the sequence's first step there
     float ld, sum_scale, last;               // last: factor of the state that is handed out
@@ -95,14 +103,19 @@ struct alignas(16) Work {
     __device__ __forceinline__ int rows(int c) const { return min(C, n - c * C); }
     __device__ __forceinline__ int late(int c) const { return c == 0 && (flags & BACK) ? 0 : 1; }
     __device__ __forceinline__ bool state(int c) const { return c > c0 || (flags & INIT); }
+    __device__ __forceinline__ bool three(int c) const { return (flags & THREE) && three_pieces(ld, n, c); }
     __device__ __forceinline__ int step(int c) const { return start + (flags & BACK ? n - c * C - rows(c) : c * C); }      // its first row
 };
 constexpr int RING = 4, ROLE_WARPS = 13;
+struct Out {                                 // where a stage's output goes: job, head, batch row, first step, steps
+    int job, h, b, t, rows;
+};
 
 struct Shared {
-    uint64_t full[4], empty[4], told[RING], heard[RING];
-    uint64_t sc_full, p_ready, k_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
+    uint64_t full[4], empty[4], staged[4], told[RING], heard[RING];
+    uint64_t sc_full, p_ready, k_ready, low_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
     Work work[RING];
+    Out out[4];
     uint32_t tmem;
     int dead;
     // weights of the scores' columns; of K's rows, in fp32 and as two bf16 pieces, rows 2 i and 2 i + 1 in word i.  (A table is written by each
@@ -252,57 +265,62 @@ __device__ __forceinline__ void k_weights(float *wk, uint32_t *wk1, uint32_t *wk
         wk2[i] = narrow(add2(pair(w[0], w[1]), wide_negative(w1)));
     }
 }
-// 32 columns of K, weighted and transposed, as three bf16 pieces: two into tensor memory (`to`, and 64 columns on), the third back to where K was
-__device__ __forceinline__ void k_pieces3(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const float *wk, int lane, int steps)
+// 32 columns of K, weighted and transposed, as two bf16 pieces in tensor memory (`to`, and 64 columns on), by bf16 arithmetic: k w1 = h + t exactly
+// (8 by 8 bits), t + k w2 rounded once.  (32 steps a turn: the loads of a turn are on their way together.)
+__device__ __forceinline__ void k_pieces(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const uint32_t *wk1, const uint32_t *wk2, int lane, int steps)
+{
+    int i = lane & 3;
+#pragma unroll 1
+    for (int j = 0; j < steps; j += 32, from += 4096, to += 16, i += 16) {
+        uint32_t k[2][2][4], w1[4], w2[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            w1[q] = wk1[i + 4 * q];
+            w2[q] = wk2[i + 4 * q];
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) ldsm4_t(from + (uint32_t)(q * 2048) + shift[g], k[q][g]);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                uint32_t h[4], m[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 kk = as_bf2(k[q][g][e]), a = as_bf2(w1[2 * q + (e >> 1)]), hh = __hmul2(kk, a);
+                    h[e] = as_word(hh);
+                    m[e] = as_word(__hfma2(kk, as_bf2(w2[2 * q + (e >> 1)]), __hfma2(kk, a, __hneg2(hh))));
+                }
+                tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 8 * q, h);
+                tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64 + 8 * q, m);
+            }
+    }
+}
+// The third piece, what the first two leave of k w in fp32, back to where K was
+__device__ __forceinline__ void k_low(uint32_t from, const uint32_t (&shift)[2], const float *wk, const uint32_t *wk1, const uint32_t *wk2, int lane, int steps)
 {
     const f2 *w = reinterpret_cast<const f2 *>(wk) + (lane & 3), minus = pair(-1.0f, -1.0f);
+    int i = lane & 3;
 #pragma unroll 1
-    for (int j = 0; j < steps; j += 16, from += 2048, to += 8, w += 8) {
+    for (int j = 0; j < steps; j += 16, from += 2048, i += 8, w += 8) {
+        const __nv_bfloat162 w1[2] = {as_bf2(wk1[i]), as_bf2(wk1[i + 4])}, w2[2] = {as_bf2(wk2[i]), as_bf2(wk2[i + 4])};
         const f2 ww[2] = {w[0], w[4]};
         uint32_t k[2][4];
         ldsm4_t(from + shift[0], k[0]);
         ldsm4_t(from + shift[1], k[1]);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            uint32_t h[4], m[4];
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                f2 y = mul2(wide(k[g][e]), ww[e >> 1]);
-                h[e] = narrow(y);
-                y = fma2(wide(h[e]), minus, y);
-                m[e] = narrow(y);
-                k[g][e] = narrow(fma2(wide(m[e]), minus, y));
+                const __nv_bfloat162 kk = as_bf2(k[g][e]), hh = __hmul2(kk, w1[e >> 1]), mm = __hfma2(kk, w2[e >> 1], __hfma2(kk, w1[e >> 1], __hneg2(hh)));
+                k[g][e] = narrow(fma2(wide(as_word(mm)), minus, fma2(wide(as_word(hh)), minus, mul2(wide(k[g][e]), ww[e >> 1]))));
             }
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16), h);
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64, m);
-            stsm4_t(from + shift[g], k[g]);
-        }
+        stsm4_t(from + shift[0], k[0]);
+        stsm4_t(from + shift[1], k[1]);
     }
     fence_proxy_async_smem();
-}
-// The same as two pieces, by bf16 arithmetic: k w1 = h + t exactly (8 by 8 bits), t + k w2 rounded once
-__device__ __forceinline__ void k_pieces2(uint32_t from, const uint32_t (&shift)[2], uint32_t to, const uint32_t *wk1, const uint32_t *wk2, int lane, int steps)
-{
-    int i = lane & 3;
-#pragma unroll 1
-    for (int j = 0; j < steps; j += 16, from += 2048, to += 8, i += 8) {
-        const __nv_bfloat162 w1[2] = {as_bf2(wk1[i]), as_bf2(wk1[i + 4])}, w2[2] = {as_bf2(wk2[i]), as_bf2(wk2[i + 4])};
-        uint32_t k[2][4];
-        ldsm4_t(from + shift[0], k[0]);
-        ldsm4_t(from + shift[1], k[1]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            uint32_t h[4], m[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const __nv_bfloat162 kk = as_bf2(k[g][e]), hh = __hmul2(kk, w1[e >> 1]);
-                h[e] = as_word(hh);
-                m[e] = as_word(__hfma2(kk, w2[e >> 1], __hfma2(kk, w1[e >> 1], __hneg2(hh))));
-            }
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16), h);
-            tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64, m);
-        }
-    }
 }
 
 // a role's place in the ring of units
@@ -341,10 +359,10 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     const uint32_t s_smem = smem_u32(base), ring = s_smem + L::S_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
     if (tid == 0) {
-        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 5); }
+        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.staged[i], 4); }
         for (int i = 0; i < RING; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.heard[i], ROLE_WARPS); }
         mbar_init(&sh.sc_full, 1); mbar_init(&sh.qs_done, 1); mbar_init(&sh.u_full, 1); mbar_init(&sh.o_full, 1);
-        mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.s_ready, 8);
+        mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.low_ready, 8); mbar_init(&sh.s_ready, 8);
         mbar_init(&sh.u_free, 8); mbar_init(&sh.o_scaled, 4); mbar_init(&sh.o_free, 4);
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -356,9 +374,26 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     const uint32_t tm = sh.tmem, lanes = tm + ((uint32_t)(quad * 32) << 16);
     if (warp == 12) {
         // ---------------------------------------------------------------- loads
-        int stage = 0, slot = 0;
+        int stage = 0, slot = 0, loads = 0;
         uint32_t par = 1, heard_par = 1;
         bool on = true;
+        // The output that a stage holds, where its Q was, goes out before Q is loaded there again: whole groups of 32 rows (the last rows of a sequence
+        // the O role has stored itself)
+        auto send = [&](int stage, uint32_t parity) {
+            on = warp_wait(sh, &sh.staged[stage], parity);
+            if (on && elect_one()) {
+                const Out o = sh.out[stage];
+                const uint32_t box = ring + (uint32_t)stage * L::STAGE + L::Q;
+                const int m = p.out_flat[o.job], hh = m & 2 ? 0 : o.h, bb = m & 1 ? 0 : o.b, Dv = p.job[o.job].Dv;
+#pragma unroll 1
+                for (int r = 0; r + 32 <= o.rows; r += 32)
+#pragma unroll 1
+                    for (int v = 0; v < Dv; v += 64) tma_store_4d(&p.out[o.job], box + (uint32_t)((v >> 6) * (C * 128) + r * 128), v, o.t + r, hh, bb);
+                bulk_commit();
+                bulk_wait_read();
+            }
+            __syncwarp();
+        };
         auto tell = [&](const Work &w) {
             on = warp_wait(sh, &sh.heard[slot], heard_par);
             if (!on) return;
@@ -392,28 +427,46 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
 #pragma unroll 1
             for (int c = w.c0; c < w.c1 && on; ++c) {
                 const int t = w.step(c);
+                const uint32_t at = ring + (uint32_t)stage * L::STAGE;
+                auto load = [&](int r, uint32_t to, int width) {
+                    const int m = p.which[w.job][r], hh = p.flat[m] & 2 ? 0 : w.h, bb = p.flat[m] & 1 ? 0 : w.b;
+#pragma unroll 1
+                    for (int d = 0; d < width; d += 64) tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
+                };
+                // Q's place (and K's, where the output is wider than Q) is given back later: the output goes out by way of it
                 on = warp_wait(sh, &sh.empty[stage], par);
                 if (!on) break;
                 if (elect_one()) {
-                    const uint32_t at = ring + (uint32_t)stage * L::STAGE;
                     mbar_expect_tx(&sh.full[stage], L::STAGE);
-#pragma unroll
-                    for (int r = 0; r < 3; ++r) {
-                        const int m = p.which[w.job][r], hh = p.flat[m] & 2 ? 0 : w.h, bb = p.flat[m] & 1 ? 0 : w.b;
-                        const uint32_t to = at + (r == 0 ? L::Q : r == 1 ? L::K : L::V);
-#pragma unroll
-                        for (int d = 0; d < (r == 2 ? DV : DK); d += 64)
-                            tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
-                    }
+                    load(2, at + L::V, DV);
+                    if (DV <= DK) load(1, at + L::K, DK);
                 }
                 __syncwarp();
+                if (loads >= L::STAGES) send(stage, par);
+                if (!on) break;
+                if (elect_one()) {
+                    sh.out[stage] = Out{w.job, w.h, w.b, t, w.rows(c)};
+                    if (DV > DK) load(1, at + L::K, DK);
+                    load(0, at + L::Q, DK);
+                }
+                __syncwarp();
+                ++loads;
                 if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
             }
         }
+        // the last outputs, oldest first
+        if (loads < L::STAGES) stage = 0;                                          // (par is then that of no load: the first of `staged` is due)
+#pragma unroll 1
+        for (int i = 0; i < min(loads, L::STAGES) && on; ++i) {
+            send(stage, loads < L::STAGES ? 0u : par);
+            if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
+        }
+        if (elect_one()) bulk_wait_all();
+        __syncwarp();
     } else if (warp == 13) {
         // ---------------------------------------------------------------- products
         int stage = 0;
-        uint32_t full_par = 0, par = 0, s_par = 0, o_par = 0;              // par: barriers that complete once a chunk
+        uint32_t full_par = 0, par = 0, s_par = 0, o_par = 0, low_par = 0; // par: barriers that complete once a chunk
         bool on = true, first = true;
         const uint32_t tmu = __shfl_sync(0xffffffffu, tm, 0);                // (known to the compiler as the same in all lanes)
         auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -432,7 +485,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             for (int c = c0; c < c1 && on; ++c) {
                 const uint32_t at = ring + (uint32_t)stage * L::STAGE;
                 const uint64_t vd = desc_mn(at + L::V, C * 128), qd = smem_desc_sw128(at + L::Q);
-                const bool state = c > c0 || (flags & INIT);
+                const bool state = c > c0 || (flags & INIT), three = __shfl_sync(0xffffffffu, (int)w.three(c), 0) != 0;
                 // columns of tensor memory by K's pieces (or P) times V.  (Rolled: the loops of all roles share one instruction cache.)
                 auto times_v = [&](uint32_t d, uint32_t a, bool add) {
 #pragma unroll 2
@@ -452,17 +505,23 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                 wait(&sh.k_ready, par);
                 if (!first) wait(&sh.u_free, par ^ 1u);
                 if (on && elect_one()) {
-                    // the small pieces first, while the sum is small: it is rounded towards zero at every step
-                    if (flags & THREE) {
-                        const uint64_t kd = desc_mn(at + L::K, C * 128);
-#pragma unroll 2
-                        for (int k = 0; k < C / 16; ++k) umma_bf16(tmu + COL_U, kd + k * K16, vd + k * K16, iv | (1u << 15), k > 0);
-                    }
-                    times_v(COL_U, COL_K + 64, flags & THREE);
+                    // (the sum is rounded towards zero at every step: the small second piece first.  The third is not there in time for that.)
+                    times_v(COL_U, COL_K + 64, false);
                     times_v(COL_U, COL_K, true);
-                    umma_commit(&sh.u_full);
+                    if (!three) umma_commit(&sh.u_full);
                 }
                 __syncwarp();
+                if (three) {
+                    wait(&sh.low_ready, low_par);
+                    low_par ^= 1u;
+                    if (on && elect_one()) {
+                        const uint64_t kd = desc_mn(at + L::K, C * 128);
+#pragma unroll 2
+                        for (int k = 0; k < C / 16; ++k) umma_bf16(tmu + COL_U, kd + k * K16, vd + k * K16, iv | (1u << 15), true);
+                        umma_commit(&sh.u_full);
+                    }
+                    __syncwarp();
+                }
                 if (!first) wait(&sh.o_free, par ^ 1u);
                 if (state) {
                     wait(&sh.s_ready, s_par);
@@ -508,50 +567,50 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                 had = -1;
                 if (more) full_f = p.job[w.job].out_scale * (w.flags & WEAK ? power_of(w.ld, (w.flags & BACK ? C - 1 - row : row) + 1 - MID) : 1.0f);
             }
-            bool stored = false;
             if (due) {
-                // By way of shared memory, where the chunk's Q was, and a tensor store of the warp's 32 rows; the sequence's last rows by plain
+                // By way of shared memory, where the chunk's Q was, and tensor stores by the loading warp; the sequence's last rows by plain
                 // stores.  (Plain stores of all rows, 16 bytes to each of 32 rows at a time, kept the load-store unit busy for 2000 cycles a chunk.)
                 const LaJob &job = p.job[out_job];
                 const int Dv = job.Dv;
                 const bool in = row < out_rows, whole = out_rows >= quad * 32 + 32;
                 if (on) on = warp_wait(sh, &sh.o_full, par ^ 1u);
                 tc_fence_after();
-                stored = whole && on;
+                const bool stored = whole && on;
                 const f2 ff = pair(out_f, out_f);
                 const uint32_t box = ring + (uint32_t)out_stage * L::STAGE + L::Q + (uint32_t)(quad * 32 * 128);
                 __nv_bfloat16 *const to = (__nv_bfloat16 *)job.o.data + out_b * job.o.batch + out_h * job.o.head + (long long)(out_t + row) * job.o.token;
 #pragma unroll 1
-                for (int v = 0; v < Dv; v += 32) {                                 // (columns beyond Dv hold something or other)
-                    uint32_t r[32];
+                for (int v = 0; v < Dv; v += 64) {                                 // (columns beyond Dv hold something or other)
+                    uint32_t r[32], q[32];
                     tmem_ld32_issue(lanes + COL_O + v, r);
+                    tmem_ld32_issue(lanes + COL_O + v + 32, q);
                     tmem_wait_ld();
-                    if (on && v + 32 >= Dv) tmem_arrive(&sh.o_free);
+                    if (on && v + 64 >= Dv) tmem_arrive(&sh.o_free);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) r[e] = narrow(mul2(pair(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), ff));
+                    for (int e = 0; e < 16; ++e) {
+                        r[e] = narrow(mul2(pair(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), ff));
+                        q[e] = narrow(mul2(pair(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1])), ff));
+                    }
                     if (stored) {
                         const uint32_t at = box + (uint32_t)((v >> 6) * (C * 128) + lane * 128);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sts128(at + ((uint32_t)((((v & 63) >> 3) + e) ^ (lane & 7)) << 4), r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
+                        for (int e = 0; e < 4; ++e) {
+                            sts128(at + ((uint32_t)(e ^ (lane & 7)) << 4), r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
+                            sts128(at + ((uint32_t)((e + 4) ^ (lane & 7)) << 4), q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]);
+                        }
                     } else if (in) {
+                        const uint4 nan = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);      // a wait gave up
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (v + 8 * e < Dv) {
-                                const uint4 y = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]), nan = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
-                                *reinterpret_cast<uint4 *>(to + v + 8 * e) = on ? y : nan;       // (a wait gave up: NaN)
-                            }
+                        for (int e = 0; e < 4; ++e) {
+                            if (v + 8 * e < Dv) *reinterpret_cast<uint4 *>(to + v + 8 * e) = on ? make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]) : nan;
+                            if (v + 32 + 8 * e < Dv) *reinterpret_cast<uint4 *>(to + v + 32 + 8 * e) = on ? make_uint4(q[4 * e], q[4 * e + 1], q[4 * e + 2], q[4 * e + 3]) : nan;
+                        }
                     }
                 }
-                if (stored) {
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        const int m = p.out_flat[out_job], hh = m & 2 ? 0 : out_h, bb = m & 1 ? 0 : out_b;
-#pragma unroll 1
-                        for (int v = 0; v < Dv; v += 64) tma_store_4d(&p.out[out_job], box + (uint32_t)((v >> 6) * (C * 128)), v, out_t + quad * 32, hh, bb);
-                        bulk_commit();
-                    }
-                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.staged[out_stage]);
+                if (++out_stage == L::STAGES) out_stage = 0;
             }
             const bool have = c < w.c1 && more;
             if (have) {
@@ -568,25 +627,34 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                         } else sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
                         __syncwarp();
                     }
-#pragma unroll 1
-                    for (int b = 0; b < 4; ++b) {
-                        // Columns of the block that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
+                    // Columns of block b that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
+                    auto kept = [&](int b) -> uint32_t {
                         const uint32_t own = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
                         const int there = rows - 32 * b;
-                        const uint32_t keep = (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) &
-                                              (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
-                        uint32_t words[16];
-                        if (back ? b < quad : b > quad) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) words[e] = 0u;
-                        } else {
-                            uint32_t s[32];
+                        return (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) & (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
+                    };
+                    if (weak) {
+#pragma unroll 1
+                        for (int b = 0; b < 4; b += 2) {                           // (two blocks' scores on their way together)
+                            uint32_t s[32], t[32], words[16];
+                            tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
+                            tmem_ld32_issue(lanes + COL_SC + 32 * b + 32, t);
+                            tmem_wait_ld();
+                            p_pack(s, words, sh.wp + 32 * b, kept(b));
+                            tmem_st16(lanes + COL_SC + 16 * b, words);
+                            p_pack(t, words, sh.wp + 32 * b + 32, kept(b + 1));
+                            tmem_st16(lanes + COL_SC + 16 * b + 16, words);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            const uint32_t keep = kept(b);
+                            uint32_t s[32], words[16];
                             tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
                             tmem_wait_ld();
-                            if (weak) p_pack(s, words, sh.wp + 32 * b, keep);
-                            else if (b != quad) {
+                            if (b != quad) {
                                 // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
-                                const float f = la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31);
+                                const float f = (back ? b > quad : b < quad) ? la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31) : 0.0f;
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
                                 p_pack(s, words, sh.wp, keep);
@@ -600,8 +668,8 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) words[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
                             }
+                            tmem_st16(lanes + COL_SC + 16 * b, words);
                         }
-                        tmem_st16(lanes + COL_SC + 16 * b, words);
                     }
                     tmem_wait_st();
                     tmem_arrive(&sh.p_ready);
@@ -626,13 +694,6 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     }
                 }
             }
-            if (due) {
-                if (lane == 0) {                                                   // the stage may be loaded again when the store has read it
-                    if (stored) bulk_wait_read();
-                    mbar_arrive(&sh.empty[out_stage]);
-                }
-                if (++out_stage == L::STAGES) out_stage = 0;
-            }
             if (!have) break;
             out_rows = w.rows(c);
             out_job = w.job;
@@ -646,7 +707,6 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             par ^= 1u;
             ++c;
         }
-        if (lane == 0) bulk_wait_all();
     } else {
         // ------------------------------------------------------------- K and S
         int stage = 0;
@@ -695,10 +755,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             for (int c = w.c0; c < w.c1; ++c) {
                 const int rows = w.rows(c);
                 if (on) on = warp_wait(sh, &sh.full[stage], full_par);
-                // (every phase of a barrier is waited for: one that is two phases behind looks as if it had completed)
-                if (on) on = warp_wait(sh, &sh.sc_full, par);                      // K as it is has met Q: the third piece takes its place
                 if (!on) break;
-                tc_fence_after();
                 if (rows != had) {                                                 // (this warp has seen the chunk before's products complete)
                     had = rows;
                     k_weights(sh.wk, sh.wk1, sh.wk2, w.ld, w.sum_scale, rows, w.flags & BACK, lane);
@@ -716,12 +773,22 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     fence_proxy_async_smem();
                     __syncwarp();
                 }
+                const float *const wk = sh.wk + half * HC;
+                const uint32_t *const wk1 = sh.wk1 + half * HC / 2, *const wk2 = sh.wk2 + half * HC / 2;
                 if (quad * 32 < DK) {
-                    if (w.flags & THREE) k_pieces3(panel + from, shift, k_to, sh.wk + half * HC, lane, HC);
-                    else k_pieces2(panel + from, shift, k_to, sh.wk1 + half * HC / 2, sh.wk2 + half * HC / 2, lane, HC);
+                    k_pieces(panel + from, shift, k_to, wk1, wk2, lane, HC);
                     tmem_wait_st();
                 }
                 tmem_arrive(&sh.k_ready);
+                // (every phase of a barrier is waited for: one that is two phases behind looks as if it had completed)
+                on = warp_wait(sh, &sh.sc_full, par);                              // K as it is has met Q: the third piece takes its place
+                if (!on) break;
+                tc_fence_after();
+                if (w.three(c)) {
+                    if (quad * 32 < DK) k_low(panel + from, shift, wk, wk1, wk2, lane, HC);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.low_ready);
+                }
                 if (w.state(c)) {
                     // the state before the chunk to shared memory, in bf16, for Q S (whose last product has met the one before it: sc_full came after)
                     if (mine) {
@@ -827,7 +894,7 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
         Unit x;
         if (!get_unit(p, u, x) || x.last) continue;
         const LaJob &job = p.job[x.job];
-        const bool back = job.back != 0, three = job.s1 != nullptr;
+        const bool back = job.back != 0;
         const float ld = p.seqs.log_decay[x.h];
         if (warp == 8) {
             // loads
@@ -854,6 +921,7 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
             const uint32_t iv = IDESC | (1u << 16) | ((uint32_t)(job.Dv >> 3) << 17);
             for (int c = x.c0; c < x.c1 && on; ++c, next()) {
                 const int s = g & 1;
+                const bool three = job.s1 != nullptr && three_pieces(ld, x.n, c);
                 const uint32_t par = (uint32_t)(g >> 1) & 1u, at = ring + (uint32_t)stage * STAGE, d = tm + STATE_U + 128 * s, a = tm + STATE_K + 128 * s;
                 on = warp_wait(sh, &sh.full[stage], full_par);
                 if (on) on = warp_wait(sh, &sh.k_ready[s], par);
@@ -890,8 +958,8 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
                 tc_fence_after();
                 if (quad * 32 < DK) {
                     const uint32_t from = panel + (uint32_t)stage * STAGE, to = lanes + STATE_K + 128 * s;
-                    if (three) k_pieces3(from, shift, to, sh.wk[quad], lane, C);
-                    else k_pieces2(from, shift, to, sh.wk1[quad], sh.wk2[quad], lane, C);
+                    k_pieces(from, shift, to, sh.wk1[quad], sh.wk2[quad], lane, C);
+                    if (job.s1 != nullptr && three_pieces(ld, x.n, c)) k_low(from, shift, sh.wk[quad], sh.wk1[quad], sh.wk2[quad], lane, C);
                     tmem_wait_st();
                 }
                 tmem_arrive(&sh.k_ready[s]);
