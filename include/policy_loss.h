@@ -31,7 +31,7 @@ extern "C" {
 #define PL_ERR_CUDA (-2)
 #define PL_F32 0
 #define PL_BF16 1
-#define PL_MAX_V (1 << 24)
+#define PL_MAX_V 200000
 
 /* type of logits and dlogits: PL_F32 or PL_BF16; actions: int64 */
 int policy_loss(const void *logits, int type, long long N, int V, long long stride, const long long *actions, const float *old_logp,

@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+from operator import attrgetter
 from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
@@ -68,10 +69,21 @@ def adamw_state(params: Sequence[torch.Tensor], bits: int = 32) -> AdamWState:
     return AdamWState(m, v, ms, vs)
 
 
+_numel, _data_ptr, _get_device, _contiguous = torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.get_device, torch.Tensor.is_contiguous
+_dtype = attrgetter("dtype")
+
+
+def _same(tensors, dtype, index, sizes, what: str):
+    """Are all of one type, on one device, contiguous, of these sizes?"""
+    if (set(map(_dtype, tensors)) != {dtype} or set(map(_get_device, tensors)) != {index} or not all(map(_contiguous, tensors))
+            or (sizes is not None and list(map(_numel, tensors)) != sizes)):
+        _bad(f"{what}: expected contiguous tensors of {dtype}, of the parameters' sizes and on their device")
+
+
 def _one(t, dtype, device, what):
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == dtype and t.numel() == 1 and t.device == device):
+    if not (t.is_cuda and t.dtype is dtype and t.numel() == 1 and t.device == device):
         _bad(f"{what}: expected one {dtype} on the parameters' device")
     return t.data_ptr()
 
@@ -100,35 +112,31 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     device, f32 = params[0].device, torch.float32
     if device.type != "cuda":
         _bad("params: expected CUDA tensors")
-    gtype = grads[0].dtype
-    if gtype not in (f32, torch.bfloat16):
+    # (the checks of many tensors go through C functions mapped over the lists: a step over 300 tensors is 300 us of kernels)
+    index, gtype = device.index, grads[0].dtype
+    if gtype is not f32 and gtype is not torch.bfloat16:
         _bad("grads: expected float32 or bfloat16")
-    sizes = [p.numel() for p in params]
-    if not all([p.dtype is f32 and p.device == device and p.is_contiguous() for p in params]):
-        _bad("params: expected contiguous float32 tensors on one device")
-    if not all([g.dtype is gtype and g.device == device and g.is_contiguous() and g.numel() == k for g, k in zip(grads, sizes)]):
-        _bad("grads: expected contiguous tensors of one type, of the parameters' sizes and on their device")
-    if copies is not None and not all([t.dtype is torch.bfloat16 and t.device == device and t.is_contiguous() and t.numel() == k
-                                       for t, k in zip(copies, sizes)]):
-        _bad("copies: expected contiguous bfloat16 tensors of the parameters' sizes and on their device")
+    sizes, pointers = list(map(_numel, params)), list(map(_data_ptr, params))
+    _same(params, f32, index, None, "params")
+    _same(grads, gtype, index, sizes, "grads")
+    if copies is not None:
+        _same(copies, torch.bfloat16, index, sizes, "copies")
     bits = 32 if m.dtype is f32 else 8
     stype, places = (f32 if bits == 32 else torch.float8_e4m3fn), _places(sizes)
     for t, what in ((m, "m"), (v, "v")):
-        if not (t.dtype is stype and t.device == device and t.is_contiguous() and t.numel() == places):
+        if not (t.dtype is stype and t.get_device() == index and t.is_contiguous() and t.numel() == places):
             _bad(f"state.{what}: expected {places} contiguous values of {stype} on the parameters' device")
-    for t, what in ((m_scale, "m_scale"), (v_scale, "v_scale")):
-        if bits == 8 and not (t is not None and t.dtype is f32 and t.device == device and t.is_contiguous() and t.numel() == places // ADAMW_BLOCK):
-            _bad(f"state.{what}: expected {places // ADAMW_BLOCK} contiguous float32 on the parameters' device")
-    table = np.zeros((n, 4), dtype=np.int64)
-    ptrs = [p.data_ptr() for p in params]
-    live = [a for a, k in zip(ptrs, sizes) if k]
+    if bits == 8:
+        for t, what in ((m_scale, "m_scale"), (v_scale, "v_scale")):
+            if not (t is not None and t.dtype is f32 and t.get_device() == index and t.is_contiguous() and t.numel() == places // ADAMW_BLOCK):
+                _bad(f"state.{what}: expected {places // ADAMW_BLOCK} contiguous float32 on the parameters' device")
+    live = pointers if 0 not in sizes else [a for a, k in zip(pointers, sizes) if k]
     if len(set(live)) != len(live):
         _bad("params: the same tensor twice")
-    table[:, 0] = ptrs
-    table[:, 1] = [g.data_ptr() for g in grads]
-    if copies is not None:
-        table[:, 2] = [t.data_ptr() for t in copies]
-    table[:, 3] = sizes
+    table = np.empty((4, n), dtype=np.int64)
+    table[0], table[1], table[3] = pointers, list(map(_data_ptr, grads)), sizes
+    table[2] = 0 if copies is None else list(map(_data_ptr, copies))
+    table = np.ascontiguousarray(table.T)
     o = _Options(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=-1 if seed is None else int(seed) & 0xFFFFFFFF)
     if isinstance(step, torch.Tensor):
         o.step_dev = _one(step, torch.int64, device, "step")

@@ -64,12 +64,34 @@ __device__ __forceinline__ unsigned mix(unsigned long long place, unsigned seed)
     x = (x ^ (x >> 16)) * 0x3C6EF373u;
     return x ^ (x >> 15);
 }
-// |y| in [0, 256) as an 8-bit float without sign, rounded by 16 random bits
-__device__ __forceinline__ unsigned cut8(float a, unsigned r)
+// Two values in a register pair, and operations on both, each rounded as its own
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float lo, float hi)
 {
-    const unsigned high = ((__float_as_uint(a) + (r << 4)) >> 20) - (120u << 3);
-    const unsigned low = (unsigned)__float2int_rd(__fadd_rn(a * 512.0f, (float)r * 0x1p-16f));
-    return a != a ? 0x7fu : a >= 0x1p-6f ? high : low;
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f2 both(float x) { return pair(x, x); }
+__device__ __forceinline__ float lo(f2 x) { return __uint_as_float((unsigned)x); }
+__device__ __forceinline__ float hi(f2 x) { return __uint_as_float((unsigned)(x >> 32)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// (two products are added one by one: packed, the compiler fuses the sum with a product, which rounds once where the formulas round twice)
+__device__ __forceinline__ f2 add_each(f2 a, f2 b) { return pair(__fadd_rn(lo(a), lo(b)), __fadd_rn(hi(a), hi(b))); }
+
+// |y| in [0, 256], finite, as an 8-bit float without sign, rounded by 16 random bits (given 16 times as large).  The lower codes count in steps of
+// 2^-9: 512 a + r / 65536, whose whole part is read off the last bits of its sum with 2^23, rounded down.
+__device__ __forceinline__ unsigned cut8(float a, unsigned r16)
+{
+    const unsigned high = (__float_as_uint(a) + r16 - (120u << 23)) >> 20;
+    const float r = __uint_as_float(0x3f800000u | (r16 << 3)) - 1.0f;
+    const unsigned low = __float_as_uint(__fadd_rd(fmaf(a, 512.0f, r), 0x1p23f)) & 0xffu;
+    return a >= 0x1p-6f ? high : low;
 }
 // four codes' values
 __device__ __forceinline__ void values8(uint32_t c, float (&x)[4])
@@ -82,19 +104,10 @@ __device__ __forceinline__ void values8(uint32_t c, float (&x)[4])
         x[2 * e + 1] = f.y;
     }
 }
-// the largest magnitude's power of two at 2^7; NaN or infinity in the block: infinity (what is read back is then NaN)
-__device__ __forceinline__ float scale_of(unsigned largest)
+// the largest magnitude's power of two at 2^7
+__device__ __forceinline__ float scale_of(float largest)
 {
-    return fmaxf(__uint_as_float(largest & 0x7f800000u) * 0x1p-7f, 0x1p-120f);
-}
-
-// One value: new moments and parameter
-__device__ __forceinline__ float update(float p, float g, float &m, float &v, float &root, const Numbers &k)
-{
-    m = __fadd_rn(__fmul_rn(m, k.b1), __fmul_rn(g, k.c1));
-    v = __fadd_rn(__fmul_rn(v, k.b2), __fmul_rn(__fmul_rn(g, g), k.c2));
-    root = __fsqrt_rn(v);
-    return __fsub_rn(__fmul_rn(p, k.keep), __fdiv_rn(__fmul_rn(m, k.lr1), __fadd_rn(__fmul_rn(root, k.rb2), k.eps)));
+    return fmaxf(__uint_as_float(__float_as_uint(largest) & 0x7f800000u) * 0x1p-7f, 0x1p-120f);
 }
 
 template <typename G>
@@ -104,17 +117,26 @@ __device__ __forceinline__ float to_f<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// One block of 256 values by a warp.  Lane: values 4 lane + 128 j + e (j < 2, e < 4); VEC: all of them exist and the parameter,
-// gradient and copy lie on the boundary of four of their values.
-template <typename G, int BITS, bool VEC>
+// How a block lies in memory: all 256 values there, the parameter, gradient and copy on the boundary of four of their values; all there; the last
+// ones of a tensor.
+enum { VECTORS, WHOLE, PART };
+
+// One block of 256 values by a warp.  Lane: values 4 lane + 128 j + e (j < 2, e < 4).
+template <typename G, int BITS, int HOW>
 __device__ __forceinline__ void block_step(float *p, const G *g, __nv_bfloat16 *copy, int left, unsigned long long place, const Call &c,
                                            const Numbers &k, float gs, bool scaled, int lane)
 {
-    float pv[2][4], gv[2][4], m[2][4], v[2][4];
+    float pv[2][4], gv[2][4], m[2][4], v[2][4], root[2][4];
+    uint32_t mc[2], vc[2];
+    float ms = 1.0f, vs = 1.0f;
+    if constexpr (BITS == 8) {
+        ms = c.m_scale[place / BLK];
+        vs = c.v_scale[place / BLK];
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int at = 128 * j + 4 * lane;
-        if constexpr (VEC) {
+        if constexpr (HOW == VECTORS) {
             const float4 a = *reinterpret_cast<const float4 *>(p + at);
             pv[j][0] = a.x; pv[j][1] = a.y; pv[j][2] = a.z; pv[j][3] = a.w;
             if constexpr (sizeof(G) == 4) {
@@ -128,13 +150,13 @@ __device__ __forceinline__ void block_step(float *p, const G *g, __nv_bfloat16 *
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const bool in = at + e < left;
+                const bool in = HOW == WHOLE || at + e < left;
                 pv[j][e] = in ? p[at + e] : 0.0f;
                 gv[j][e] = in ? to_f<G>(g[at + e]) : 0.0f;
             }
         }
         if constexpr (BITS == 32) {
-            if (VEC || left >= BLK) {              // the state's places lie on multiples of 256
+            if constexpr (HOW != PART) {           // the state's places lie on multiples of 256
                 const float4 a = *reinterpret_cast<const float4 *>((const float *)c.m + place + at);
                 const float4 b = *reinterpret_cast<const float4 *>((const float *)c.v + place + at);
                 m[j][0] = a.x; m[j][1] = a.y; m[j][2] = a.z; m[j][3] = a.w;
@@ -148,51 +170,50 @@ __device__ __forceinline__ void block_step(float *p, const G *g, __nv_bfloat16 *
                 }
             }
         } else {
-            values8(*reinterpret_cast<const uint32_t *>((const uint8_t *)c.m + place + at), m[j]);
-            values8(*reinterpret_cast<const uint32_t *>((const uint8_t *)c.v + place + at), v[j]);
+            mc[j] = *reinterpret_cast<const uint32_t *>((const uint8_t *)c.m + place + at);
+            vc[j] = *reinterpret_cast<const uint32_t *>((const uint8_t *)c.v + place + at);
         }
     }
-    float ms = 1.0f, vs = 1.0f;
-    if constexpr (BITS == 8) {
-        ms = c.m_scale[place / BLK];
-        vs = c.v_scale[place / BLK];
-    }
-    float root[2][4];
-    unsigned mb = 0, vb = 0;
+    float mb = 0.0f;
+    unsigned vb = 0;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+        if constexpr (BITS == 8) {
+            values8(mc[j], m[j]);
+            values8(vc[j], v[j]);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 4; e += 2) {
+            f2 g2 = pair(gv[j][e], gv[j][e + 1]), m2 = pair(m[j][e], m[j][e + 1]), v2 = pair(v[j][e], v[j][e + 1]);
+            if (scaled) g2 = mul2(g2, both(gs));
             if constexpr (BITS == 8) {
-                m[j][e] *= ms;
-                v[j][e] *= vs;
-                v[j][e] = __fmul_rn(v[j][e], v[j][e]);
+                m2 = mul2(m2, both(ms));
+                v2 = mul2(v2, both(vs));
+                v2 = mul2(v2, v2);
             }
-            const float gg = scaled ? __fmul_rn(gv[j][e], gs) : gv[j][e];
-            pv[j][e] = update(pv[j][e], gg, m[j][e], v[j][e], root[j][e], k);
-            if (BITS == 8 && (VEC || 128 * j + 4 * lane + e < left)) {
-                mb = max(mb, __float_as_uint(m[j][e]) & 0x7fffffffu);
-                vb = max(vb, __float_as_uint(root[j][e]) & 0x7fffffffu);
-            }
-        }
-    float mi = 1.0f, vi = 1.0f;
-    if constexpr (BITS == 8) {
-        mb = __reduce_max_sync(0xffffffffu, mb);
-        vb = __reduce_max_sync(0xffffffffu, vb);
-        ms = scale_of(mb);
-        vs = scale_of(vb);
-        mi = 1.0f / ms;                            // powers of two: exact
-        vi = 1.0f / vs;
-        __syncwarp();                              // every lane has read the old scales
-        if (lane == 0) {
-            c.m_scale[place / BLK] = ms;
-            c.v_scale[place / BLK] = vs;
+            m2 = add_each(mul2(m2, both(k.b1)), mul2(g2, both(k.c1)));
+            v2 = add_each(mul2(v2, both(k.b2)), mul2(mul2(g2, g2), both(k.c2)));
+            m[j][e] = lo(m2); m[j][e + 1] = hi(m2);
+            v[j][e] = lo(v2); v[j][e + 1] = hi(v2);
+            root[j][e] = __fsqrt_rn(v[j][e]);
+            root[j][e + 1] = __fsqrt_rn(v[j][e + 1]);
+            const f2 under = add_each(mul2(pair(root[j][e], root[j][e + 1]), both(k.rb2)), both(k.eps)), over = mul2(m2, both(k.lr1));
+            const f2 kept = mul2(pair(pv[j][e], pv[j][e + 1]), both(k.keep));
+            pv[j][e] = __fsub_rn(lo(kept), __fdiv_rn(lo(over), lo(under)));
+            pv[j][e + 1] = __fsub_rn(hi(kept), __fdiv_rn(hi(over), hi(under)));
+            if constexpr (BITS == 8)
+#pragma unroll
+                for (int i = e; i < e + 2; ++i)
+                    if (HOW != PART || 128 * j + 4 * lane + i < left) {
+                        mb = fmaxf(mb, fabsf(m[j][i]));
+                        vb = max(vb, __float_as_uint(root[j][i]));     // (not negative; a NaN is the largest)
+                    }
         }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int at = 128 * j + 4 * lane;
-        if constexpr (VEC) {
+        if constexpr (HOW == VECTORS) {
             *reinterpret_cast<float4 *>(p + at) = make_float4(pv[j][0], pv[j][1], pv[j][2], pv[j][3]);
             if (copy != nullptr) {
                 const __nv_bfloat162 a = __floats2bfloat162_rn(pv[j][0], pv[j][1]), b = __floats2bfloat162_rn(pv[j][2], pv[j][3]);
@@ -201,13 +222,13 @@ __device__ __forceinline__ void block_step(float *p, const G *g, __nv_bfloat16 *
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (at + e < left) {
+                if (HOW == WHOLE || at + e < left) {
                     p[at + e] = pv[j][e];
                     if (copy != nullptr) copy[at + e] = __float2bfloat16_rn(pv[j][e]);
                 }
         }
         if constexpr (BITS == 32) {
-            if (VEC || left >= BLK) {
+            if constexpr (HOW != PART) {
                 *reinterpret_cast<float4 *>((float *)c.m + place + at) = make_float4(m[j][0], m[j][1], m[j][2], m[j][3]);
                 *reinterpret_cast<float4 *>((float *)c.v + place + at) = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
             } else {
@@ -218,26 +239,42 @@ __device__ __forceinline__ void block_step(float *p, const G *g, __nv_bfloat16 *
                         ((float *)c.v)[place + at + e] = v[j][e];
                     }
             }
-        } else {
-            uint32_t mc = 0, vc = 0;
+        }
+    }
+    if constexpr (BITS == 8) {
+        mb = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mb)));      // (every lane has read the old scales before this)
+        vb = __reduce_max_sync(0xffffffffu, vb);
+        const bool fine = vb < 0x7f800000u && mb < INFINITY;       // a gradient that is not finite shows in v, whatever it does to m
+        ms = fine ? scale_of(mb) : 1.0f;
+        vs = fine ? scale_of(__uint_as_float(vb)) : 1.0f;
+        const float mi = 1.0f / ms, vi = 1.0f / vs;                // powers of two: exact
+        if (lane == 0) {
+            c.m_scale[place / BLK] = ms;
+            c.v_scale[place / BLK] = vs;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = 128 * j + 4 * lane;
+            unsigned mq = 0, vq = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const unsigned r = mix(place + at + e, k.seed);
                 const float y = m[j][e] * mi;
-                mc |= (cut8(fabsf(y), r & 0xffffu) | (__float_as_uint(y) >> 31 << 7)) << (8 * e);
-                unsigned q = cut8(root[j][e] * vi, r >> 16);
-                if (q == 0 && root[j][e] > 0.0f) q = 1;
-                vc |= q << (8 * e);
+                const unsigned q = cut8(fabsf(y), (r << 4) & 0xffff0u) | ((__float_as_uint(y) >> 24) & 0x80u);
+                const unsigned w = max(cut8(root[j][e] * vi, (r >> 12) & 0xffff0u), root[j][e] > 0.0f ? 1u : 0u);
+                mq |= q << (8 * e);
+                vq |= w << (8 * e);
             }
-            if (VEC || at + 4 <= left) {
-                *reinterpret_cast<uint32_t *>((uint8_t *)c.m + place + at) = mc;
-                *reinterpret_cast<uint32_t *>((uint8_t *)c.v + place + at) = vc;
+            if (!fine) mq = vq = 0x7f7f7f7fu;                      // the block is NaN
+            if (HOW != PART || at + 4 <= left) {
+                *reinterpret_cast<uint32_t *>((uint8_t *)c.m + place + at) = mq;
+                *reinterpret_cast<uint32_t *>((uint8_t *)c.v + place + at) = vq;
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (at + e < left) {
-                        ((uint8_t *)c.m)[place + at + e] = (uint8_t)(mc >> (8 * e));
-                        ((uint8_t *)c.v)[place + at + e] = (uint8_t)(vc >> (8 * e));
+                        ((uint8_t *)c.m)[place + at + e] = (uint8_t)(mq >> (8 * e));
+                        ((uint8_t *)c.v)[place + at + e] = (uint8_t)(vq >> (8 * e));
                     }
             }
         }
@@ -279,8 +316,9 @@ __global__ void __launch_bounds__(TH) adamw_kernel(const __grid_constant__ Table
         const unsigned long long place = (unsigned long long)t.block[lo] * BLK + at;
         const int left = (int)min((long long)BLK, n - at);
         __nv_bfloat16 *const cp = copy != nullptr ? copy + at : nullptr;
-        if (four && left == BLK) block_step<G, BITS, true>(p + at, g + at, cp, left, place, c, k, gs, scaled, lane);
-        else block_step<G, BITS, false>(p + at, g + at, cp, left, place, c, k, gs, scaled, lane);
+        if (left < BLK) block_step<G, BITS, PART>(p + at, g + at, cp, left, place, c, k, gs, scaled, lane);
+        else if (four) block_step<G, BITS, VECTORS>(p + at, g + at, cp, left, place, c, k, gs, scaled, lane);
+        else block_step<G, BITS, WHOLE>(p + at, g + at, cp, left, place, c, k, gs, scaled, lane);
     }
 }
 

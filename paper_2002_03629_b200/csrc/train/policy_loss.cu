@@ -3,9 +3,10 @@
 // Bound: memory, the logits read once and the gradient written once; next the exponentials, two for every logit, which the special
 // function unit makes at 16 a cycle and SM.  A row is read in pieces of 16 bytes that lie on 16 bytes: rows of odd length begin and end
 // inside a piece, whose values are then read one by one.
-//   rows_kernel     a row's pieces stay in the registers of 32 to 512 threads: read once from anywhere
-//   stream_kernel   longer rows: one pass with the running maximum and sum, a second one that finds the row in L2.  Few long rows are shared
-//                   by the CTAs of a cluster, which exchange maximum and sum through distributed shared memory.
+//   rows_kernel   a row's pieces stay in the registers of 32 or 256 threads
+//   ring_kernel   longer rows: a persistent CTA keeps a ring of rows in shared memory, filled by bulk copies, so that the next rows are on their
+//                 way while one is summed and its gradient written.  Rows that leave no room for two, and few rows, are shared by the CTAs of a
+//                 cluster, which exchange maximum and sum through distributed shared memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -15,6 +16,7 @@
 #include <cstdio>
 
 #include "../../../include/policy_loss.h"
+#include "../tc_common.cuh"
 
 namespace {
 
@@ -81,16 +83,15 @@ __device__ __forceinline__ Piece<T> load_piece(const T *row, int first, int V)
     }
     return p;
 }
-// ALIKE: the row to write lies against 16 bytes as the one that was read
+// alike: the row to write lies against 16 bytes as the one that was read
 template <typename T>
-__device__ __forceinline__ void store_piece(T *row, int first, int V, const float (&x)[Piece<T>::W], bool alike)
+__device__ __forceinline__ void store_piece(T *row, int first, int V, const Piece<T> &p, bool alike)
 {
     constexpr int W = Piece<T>::W;
-    if (alike && first >= 0 && first + W <= V) {
-        Piece<T> p;
-        p.set(x);
-        __stcs(reinterpret_cast<uint4 *>(row + first), p.raw);
-    } else {
+    if (alike && first >= 0 && first + W <= V) __stcs(reinterpret_cast<uint4 *>(row + first), p.raw);
+    else {
+        float x[W];
+        p.get(x);                                      // (rounded already: the way back to the type changes nothing)
 #pragma unroll
         for (int e = 0; e < W; ++e)
             if (first + e >= 0 && first + e < V) put(row + first + e, x[e]);
@@ -102,13 +103,91 @@ __device__ __forceinline__ int lead(const T *row)      // values between the 16-
     return (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
 }
 
-// e^(z - m).  bf16 gradients: the special function's 2^x, off by 2^-22; fp32 keeps the full precision.
+// Exponentials against a reference.  fp32 logits: e^(z - m) to full precision.  bf16 logits: 2^(z log2 e - M) by the special function, off by 2^-22,
+// with M = m log2 e as rounded: the same M stands in the action's own logarithm, so that its rounding cancels.
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 template <typename T>
-__device__ __forceinline__ float exp_of(float z, float m)
+__device__ __forceinline__ float reference(float m)
 {
-    if constexpr (sizeof(T) == 4) return expf(z - m);
-    else return exp2f((z - m) * 1.44269504088896341f);
+    if constexpr (sizeof(T) == 4) return m;
+    else return m * LOG2E;
 }
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <typename T>
+__device__ __forceinline__ float exp_of(float z, float ref)
+{
+    if constexpr (sizeof(T) == 4) return expf(z - ref);
+    else return power2(fmaf(z, LOG2E, -ref));
+}
+// z - log sum exp, for the sum s against the reference
+template <typename T>
+__device__ __forceinline__ float log_share(float z, float ref, float s)
+{
+    if constexpr (sizeof(T) == 4) return z - ref - logf(s);
+    else return (fmaf(z, LOG2E, -ref) - log2f(s)) * LN2;
+}
+
+// What is done with a piece: its maximum (NaN aside), the sum of its exponentials, and those as a piece of the gradient.  (Packed operations on two
+// fp32 values save nothing here: bringing the values into pairs costs what they save.)
+template <typename T>
+__device__ __forceinline__ float piece_max(const Piece<T> &p)
+{
+    if constexpr (sizeof(T) == 4) {
+        float x[4];
+        p.get(x);
+        return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    } else {
+        const __nv_bfloat162 *w = reinterpret_cast<const __nv_bfloat162 *>(&p.raw);
+        const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+}
+// (two sums, so that an addition need not wait for the one before)
+template <typename T>
+__device__ __forceinline__ void piece_sum(const Piece<T> &p, float ref, float (&sum)[2])
+{
+    constexpr int W = Piece<T>::W;
+    float x[W];
+    p.get(x);
+#pragma unroll
+    for (int e = 0; e < W; ++e) sum[e & 1] += exp_of<T>(x[e], ref);
+}
+// What the gradient's exponentials count against.  fp32: the reference, and a factor -g / sum.  bf16: the factor's logarithm in the reference, its sign
+// put on afterwards, two values at a time.
+struct Against {
+    float ref, factor;
+    uint32_t sign;
+};
+template <typename T>
+__device__ __forceinline__ Against gradient_against(float ref, float g, float sum)
+{
+    const float factor = -g / sum;
+    if constexpr (sizeof(T) == 4) return Against{ref, factor, 0u};
+    else return Against{ref - log2f(fabsf(factor)), 1.0f, factor < 0.0f ? 0x80008000u : 0u};
+}
+template <typename T>
+__device__ __forceinline__ Piece<T> piece_gradient(const Piece<T> &p, const Against &a)
+{
+    constexpr int W = Piece<T>::W;
+    Piece<T> out;
+    float x[W];
+    p.get(x);
+#pragma unroll
+    for (int e = 0; e < W; ++e) x[e] = sizeof(T) == 4 ? exp_of<T>(x[e], a.ref) * a.factor : exp_of<T>(x[e], a.ref);
+    out.set(x);
+    if constexpr (sizeof(T) == 2) {
+        out.raw.x ^= a.sign; out.raw.y ^= a.sign; out.raw.z ^= a.sign; out.raw.w ^= a.sign;
+    }
+    return out;
+}
+// the action's own value: g on top, rounded once
+template <typename T>
+__device__ __forceinline__ void put_action(const Call &c, T *dz, int action, float za, float ref, float sum, float g) { put(dz + action, fmaf(exp_of<T>(za, ref), -g / sum, g)); }
 
 // A running maximum and the sum of exponentials against it.  While nothing but -infinity has been seen the sum counts against 0.
 struct Sum {
@@ -118,56 +197,55 @@ __device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.0f
 template <typename T>
 __device__ __forceinline__ Sum join(Sum a, Sum b)
 {
-    const float m = fmaxf(a.m, b.m), t = against(m);
-    // (a side that has seen nothing has sum 0; a NaN in a sum stays)
-    return Sum{m, (a.m == m ? a.s : a.s * exp_of<float>(a.m, t)) + (b.m == m ? b.s : b.s * exp_of<float>(b.m, t))};
+    const float m = fmaxf(a.m, b.m), r = reference<T>(against(m));
+    // (a side that has seen nothing has sum 0; a NaN in a sum stays.  Sums count against the reference of their own maximum: the factor is the
+    // quotient of the two references, not of the maxima)
+    auto moved = [&](Sum x) {
+        if (x.m == m) return x.s;
+        if constexpr (sizeof(T) == 4) return x.s * expf(against(x.m) - r);
+        else return x.s * exp2f(reference<T>(against(x.m)) - r);
+    };
+    return Sum{m, moved(a) + moved(b)};
 }
-template <typename T>
-__device__ __forceinline__ Sum join_warp(Sum a)
-{
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) a = join<T>(a, Sum{__shfl_xor_sync(0xffffffffu, a.m, d), __shfl_xor_sync(0xffffffffu, a.s, d)});
-    return a;
-}
-
 // What a row's loss and gradient are made of
 struct Row {
     float loss, logp, g;                   // g = d loss / d logp
     bool blank;                            // weight 0
 };
+struct Given {                             // what the call says of a row; za: the action's logit (0 if there is no such symbol)
+    float w, adv, old, ref, za;
+    bool known;
+};
 template <typename T>
-__device__ __forceinline__ Row row_numbers(const Call &c, long long i, Sum a, const T *z, long long action)
+__device__ __forceinline__ Given given(const Call &c, long long i, const T *z, long long action)
+{
+    Given g;
+    g.known = action >= 0 && action < c.V;
+    g.w = c.w != nullptr ? c.w[i] : c.each;
+    g.adv = c.adv[i];
+    g.old = c.old_logp[i];
+    g.ref = c.ref != nullptr ? c.ref[i] : 0.0f;
+    g.za = g.known ? value(z + action) : 0.0f;
+    return g;
+}
+template <typename T>
+__device__ __forceinline__ Row row_numbers(const Call &c, const Given &x, float ref, float sum)
 {
     Row r;
-    const float w = c.w != nullptr ? c.w[i] : c.each;
-    const bool known = action >= 0 && action < c.V;
-    r.logp = known ? value(z + action) - a.m - logf(a.s) : NAN;
-    const float A = c.adv[i], ratio = expf(r.logp - c.old_logp[i]);
-    const float u = ratio * A, held = fminf(fmaxf(ratio, c.lo), c.hi) * A;
+    r.logp = x.known ? log_share<T>(x.za, ref, sum) : NAN;
+    const float ratio = expf(r.logp - x.old);
+    const float u = ratio * x.adv, held = fminf(fmaxf(ratio, c.lo), c.hi) * x.adv;
     // (a NaN on either side has to come out)
     float loss = u != u ? u : -fminf(u, held), g = u <= held ? -u : u != u ? u : 0.0f;
     if (c.ref != nullptr) {
-        const float d = c.ref[i] - r.logp, x = expm1f(d);
-        loss = fmaf(c.kl, x - d, loss);
-        g = fmaf(-c.kl, x, g);
+        const float d = x.ref - r.logp, y = expm1f(d);
+        loss = fmaf(c.kl, y - d, loss);
+        g = fmaf(-c.kl, y, g);
     }
-    r.blank = w == 0.0f;
-    r.loss = r.blank ? 0.0f : loss * w;
-    r.g = r.blank ? 0.0f : g * w;
+    r.blank = x.w == 0.0f;
+    r.loss = r.blank ? 0.0f : loss * x.w;
+    r.g = r.blank ? 0.0f : g * x.w;
     return r;
-}
-// gradient of W values from `first` on
-template <typename T>
-__device__ __forceinline__ void gradient(const Piece<T> &p, int first, int action, const Row &r, float m, float factor, float (&out)[Piece<T>::W])
-{
-    float x[Piece<T>::W];
-    p.get(x);
-#pragma unroll
-    for (int e = 0; e < Piece<T>::W; ++e) {
-        float d = exp_of<T>(x[e], m) * factor;
-        if (first + e == action) d += r.g;
-        out[e] = r.blank ? 0.0f : d;
-    }
 }
 
 // G threads to a row, K pieces each in registers
@@ -188,16 +266,11 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) rows_kernel(const __grid_co
         if (first < c.V) p[k] = load_piece(z, first, c.V);
     }
     const long long action = c.actions[i];
-    Sum a{-INFINITY, 0.0f};
+    const Given x = given(c, i, z, action);            // (before any thread of the row writes: dlogits may be the logits)
+    float m = -INFINITY;                    // the row's maximum
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (from + (k * G + t) * W >= c.V) continue;
-        float x[W];
-        p[k].get(x);
-#pragma unroll
-        for (int e = 0; e < W; ++e) a.m = fmaxf(a.m, x[e]);
-    }
-    float m = a.m;                          // the row's maximum
+    for (int k = 0; k < K; ++k)
+        if (from + (k * G + t) * W < c.V) m = fmaxf(m, piece_max<T>(p[k]));
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     if constexpr (G > 32) {
@@ -206,29 +279,25 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) rows_kernel(const __grid_co
 #pragma unroll
         for (int w = 0; w < G / 32; ++w) m = fmaxf(m, sums[w].m);
     }
-    a.m = m;
-    m = against(m);
+    // (a row of nothing but -infinity has the sum 0: its logarithm, -infinity - (-infinity), is NaN)
+    const float ref = reference<T>(against(m));
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (from + (k * G + t) * W >= c.V) continue;
-        float x[W];
-        p[k].get(x);
+    for (int k = 0; k < K; ++k)
+        if (from + (k * G + t) * W < c.V) piece_sum<T>(p[k], ref, sum);
+    float total = sum[0] + sum[1];
 #pragma unroll
-        for (int e = 0; e < W; ++e) a.s += exp_of<T>(x[e], m);
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    __syncwarp();
     if constexpr (G > 32) {
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5].s = a.s;
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5].s = total;
         __syncthreads();
-        a.s = 0.0f;
+        total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < G / 32; ++w) a.s += sums[w].s;
+        for (int w = 0; w < G / 32; ++w) total += sums[w].s;
     }
-    const Row r = row_numbers<T>(c, i, a, z, action);
-    if constexpr (G > 32) __syncthreads();      // every thread has read its action's logit: dlogits may be the logits
-    else __syncwarp();
+    const Row r = row_numbers<T>(c, x, ref, total);
     if (t == 0) {
         c.loss[i] = r.loss;
         c.logp[i] = r.logp;
@@ -236,104 +305,161 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) rows_kernel(const __grid_co
     if (c.dz == nullptr) return;
     T *const dz = (T *)c.dz + i * c.dstride;
     const bool alike = lead(dz) == -from;
-    const float factor = -r.g / a.s;
+    const Against g = gradient_against<T>(ref, r.g, total);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int first = from + (k * G + t) * W;
         if (first >= c.V) continue;
-        float d[W];
-        gradient<T>(p[k], first, (int)action, r, m, factor, d);
+        Piece<T> d;
+        d.raw = make_uint4(0, 0, 0, 0);
+        if (!r.blank) d = piece_gradient<T>(p[k], g);
         store_piece(dz, first, c.V, d, alike);
+        if (!r.blank && x.known && (unsigned long long)(action - first) < (unsigned long long)W) put_action<T>(c, dz, (int)action, x.za, ref, total, r.g);
     }
 }
 
-constexpr int STH = 512;
+constexpr int RTH = 512, RING = 8;
+constexpr int RING_BYTES = 108 * 1024;
+struct RingShared {
+    uint64_t full[RING];
+    float top[RTH / 32], sum[RTH / 32];
+    Sum cta[2][8];
+    Row row;
+    Against against;
+    float ref, total;
+    int dead;
+};
 
-// Long rows: a cluster of CTAs to a row, its pieces dealt to them in turn
+// Long rows: a cluster of `ctas` CTAs takes a row at a time, `per` pieces each, and keeps `bufs` of its rows in shared memory
 template <typename T>
-__global__ void __launch_bounds__(STH, 2) stream_kernel(const __grid_constant__ Call c, int ctas)
+__global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Call c, int ctas, int per, int bufs)
 {
-    constexpr int W = Piece<T>::W, U = 4;
-    __shared__ Sum sums[STH / 32], all, shared[8];
-    const int tid = threadIdx.x;
-    uint32_t rank;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    const long long i = blockIdx.x / ctas;
-    const T *const z = (const T *)c.z + i * c.stride;
-    const int from = -lead(z), step = ctas * STH * W;
-    const long long action = c.actions[i];
-    Sum a{-INFINITY, 0.0f};
-#pragma unroll 1
-    for (long long f = from + ((int)rank * STH + tid) * W; f < c.V; f += (long long)U * step) {
-        Piece<T> p[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) p[u] = f + (long long)u * step < c.V ? load_piece(z, (int)f + u * step, c.V) : Piece<T>{};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (f + (long long)u * step >= c.V) continue;
-            float x[W], top = a.m;
-            p[u].get(x);
-#pragma unroll
-            for (int e = 0; e < W; ++e) top = fmaxf(top, x[e]);
-            if (top > a.m) {
-                if (a.m != -INFINITY) a.s *= exp_of<float>(a.m, top);
-                a.m = top;
-            }
-            const float m = against(a.m);
-#pragma unroll
-            for (int e = 0; e < W; ++e) a.s += exp_of<T>(x[e], m);
-        }
+    constexpr int W = Piece<T>::W;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ RingShared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = ctas > 1 ? (int)cluster_rank() : 0;
+    const long long first_row = blockIdx.x / ctas, rows = gridDim.x / ctas;
+    // A row's pieces that this CTA takes, and those of them that lie in the row from end to end: they come by bulk copy
+    auto load = [&](long long i, int buf) {
+        const T *const z = (const T *)c.z + i * c.stride;
+        const int from = -lead(z), pieces = (c.V - from + W - 1) / W;
+        const int p0 = rank * per, p1 = min(p0 + per, pieces);
+        const int q0 = max(p0, from < 0 ? 1 : 0), q1 = min(p1, (c.V - from) / W);
+        const uint32_t bytes = q1 > q0 ? (uint32_t)(q1 - q0) * 16u : 0u;
+        mbar_expect_tx(&sh.full[buf], bytes);
+        if (bytes) bulk_load(smem_u32(ring) + (uint32_t)((buf * per + q0 - p0) * 16), z + from + (long long)q0 * W, bytes, &sh.full[buf]);
+    };
+    if (tid == 0) {
+        for (int i = 0; i < bufs; ++i) mbar_init(&sh.full[i], 1);
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int k = 0; k < bufs; ++k)
+            if (first_row + k * rows < c.N) load(first_row + k * rows, k);
     }
-    a = join_warp<T>(a);
-    if ((tid & 31) == 0) sums[tid >> 5] = a;
     __syncthreads();
-    if (tid < 32) {
-        a = join_warp<T>(tid < STH / 32 ? sums[tid] : Sum{-INFINITY, 0.0f});
+    if (ctas > 1) cluster_sync();                          // every CTA's shared memory is there to be written to
+    int buf = 0, turn = 0;
+    uint32_t par = 0;
+    for (long long i = first_row; i < c.N; i += rows, turn ^= 1) {
+        const T *const z = (const T *)c.z + i * c.stride;
+        const int from = -lead(z), p0 = rank * per, p1 = min(p0 + per, (c.V - from + W - 1) / W);
+        const long long action = c.actions[i];
+        Given x{};                                          // (asked for now, needed later; and before anything of the row is written: dlogits may be
+        if (tid == 0) x = given(c, i, z, action);          // the logits)
+        // (a wait for this CTA's own copies: it ends, at the latest after MBAR_WAIT_NS, and then the row is NaN)
+        bool here = mbar_try_wait(&sh.full[buf], par);
+        if (!here) {
+            const uint64_t t0 = global_ns();
+            while (!(here = mbar_try_wait(&sh.full[buf], par)) && global_ns() - t0 < MBAR_WAIT_NS) {}
+        }
+        // pieces that lie in the row from end to end, in shared memory; the row's first and last one may be a part, which one thread each reads
+        const int q0 = max(p0, from < 0 ? 1 : 0), q1 = max(q0, min(p1, (c.V - from) / W));
+        const uint4 *const mine = reinterpret_cast<const uint4 *>(ring + (size_t)buf * per * 16) + (q0 - p0) + tid;
+        const int count = (q1 - q0 - tid + RTH - 1) / RTH;                // this thread's
+        const int edge = tid == 0 && p0 < q0 && p0 < p1 ? p0 : tid == 32 && q1 < p1 && q1 >= q0 && (q1 > p0 || q0 == p0) ? q1 : -1;
+        Piece<T> part;
+        if (edge >= 0) part = load_piece(z, from + edge * W, c.V);
+        // The maximum first: a running one would be raised by some lane of a warp at nearly every piece, and each time costs more than the pieces do
+        float m = edge >= 0 ? piece_max<T>(part) : -INFINITY;
+#pragma unroll 4
+        for (int k = 0; k < count; ++k) m = fmaxf(m, piece_max<T>(Piece<T>{mine[k * RTH]}));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        if (lane == 0) sh.top[warp] = m;
+        __syncthreads();
+        m = sh.top[lane % (RTH / 32)];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        float ref = reference<T>(against(m));
+        float sums[2] = {0.0f, 0.0f};
+        if (edge >= 0) piece_sum<T>(part, ref, sums);
+#pragma unroll 2
+        for (int k = 0; k < count; ++k) piece_sum<T>(Piece<T>{mine[k * RTH]}, ref, sums);
+        float sum = sums[0] + sums[1];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) sh.sum[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+            sum = lane < RTH / 32 ? sh.sum[lane] : 0.0f;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (!here) sum = NAN;
+        }
         if (ctas > 1) {
             // every CTA of the cluster gets every other one's sum, and adds them in the same order
             if (tid < ctas) {
-                const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&shared[rank]);
-                uint32_t there;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(tid));
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(a.m), "f"(a.s) : "memory");
+                const uint32_t there = peer_addr(smem_u32(&sh.cta[turn][rank]), (uint32_t)tid);
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(m), "f"(sum) : "memory");
             }
-        } else if (tid == 0) all = a;
-    }
-    if (ctas > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            cluster_sync();
+        }
         if (tid == 0) {
-            Sum b = shared[0];
-            for (int k = 1; k < ctas; ++k) b = join<T>(b, shared[k]);
-            all = b;
+            Sum all{m, sum};
+            if (ctas > 1) {
+                all = sh.cta[turn][0];
+                for (int k = 1; k < ctas; ++k) all = join<T>(all, sh.cta[turn][k]);
+            }
+            sh.ref = reference<T>(against(all.m));
+            const Row r = row_numbers<T>(c, x, sh.ref, all.s);
+            if (rank == 0) {
+                c.loss[i] = r.loss;
+                c.logp[i] = r.logp;
+            }
+            sh.row = r;
+            sh.total = all.s;
+            sh.against = gradient_against<T>(sh.ref, r.g, all.s);
         }
-    }
-    __syncthreads();
-    a = all;
-    const Row r = row_numbers<T>(c, i, a, z, action);
-    // dlogits may be the logits: every thread of the cluster has read its action's logit
-    if (ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    else __syncthreads();
-    if (tid == 0 && rank == 0) {
-        c.loss[i] = r.loss;
-        c.logp[i] = r.logp;
-    }
-    if (c.dz == nullptr) return;
-    T *const dz = (T *)c.dz + i * c.dstride;
-    const bool alike = lead(dz) == -from;
-    const float m = against(a.m), factor = -r.g / a.s;
-#pragma unroll 1
-    for (long long f = from + ((int)rank * STH + tid) * W; f < c.V; f += (long long)U * step) {
-        Piece<T> p[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) p[u] = f + (long long)u * step < c.V ? load_piece(z, (int)f + u * step, c.V) : Piece<T>{};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (f + (long long)u * step >= c.V) continue;
-            float d[W];
-            gradient<T>(p[u], (int)f + u * step, (int)action, r, m, factor, d);
-            store_piece(dz, (int)f + u * step, c.V, d, alike);
+        __syncthreads();
+        const Row r = sh.row;
+        ref = sh.ref;
+        if (c.dz != nullptr) {
+            T *const dz = (T *)c.dz + i * c.dstride;
+            const bool alike = lead(dz) == -from;
+            const Against g = sh.against;
+            const Piece<T> zero{make_uint4(0, 0, 0, 0)};
+            T *const to = dz + from + (q0 + tid) * W;
+            if (edge >= 0) store_piece(dz, from + edge * W, c.V, r.blank ? zero : piece_gradient<T>(part, g), alike);
+            if (alike) {
+                if (r.blank)
+                    for (int k = 0; k < count; ++k) __stcs(reinterpret_cast<uint4 *>(to + k * RTH * W), zero.raw);
+                else
+#pragma unroll 2
+                    for (int k = 0; k < count; ++k) __stcs(reinterpret_cast<uint4 *>(to + k * RTH * W), piece_gradient<T>(Piece<T>{mine[k * RTH]}, g).raw);
+            } else
+                for (int k = 0; k < count; ++k)
+                    store_piece(dz, from + (q0 + tid + k * RTH) * W, c.V, r.blank ? zero : piece_gradient<T>(Piece<T>{mine[k * RTH]}, g), false);
         }
+        __syncthreads();                                   // the buffer has been read, sh too; the action's value may be put over
+        if (tid == 0 && c.dz != nullptr && !r.blank && x.known) {
+            const int k = ((int)action - from) / W;
+            if (k >= p0 && k < p1) put_action<T>(c, (T *)c.dz + i * c.dstride, (int)action, x.za, sh.ref, sh.total, r.g);
+        }
+        if (tid == 0 && i + bufs * rows < c.N) load(i + bufs * rows, buf);
+        if (++buf == bufs) { buf = 0; par ^= 1u; }
     }
+    if (ctas > 1) cluster_sync();
 }
 
 int launched()
@@ -361,20 +487,26 @@ int launch(const Call &c, cudaStream_t stream)
     else if (pieces <= 32 * 5) rows_kernel<T, 32, 5><<<(rows + 7) / 8, 256, 0, stream>>>(c);
     else if (pieces <= 256 * 2) rows_kernel<T, 256, 2><<<rows, 256, 0, stream>>>(c);
     else if (pieces <= 256 * 5) rows_kernel<T, 256, 5><<<rows, 256, 0, stream>>>(c);
-    else if (pieces <= 512 * 5) rows_kernel<T, 512, 5><<<rows, 512, 0, stream>>>(c);
     else {
+        // CTAs to a row: so many that a slice fits into shared memory, and that few rows find all SMs (a slice of two pieces a thread at least)
+        const long long sms = sm_count();
         int ctas = 1;
-        while (ctas < 8 && c.N * ctas * 2 <= 2ll * sm_count() && pieces > 2 * ctas * STH) ctas *= 2;
+        while (ctas < 8 && (16ll * ((pieces + ctas - 1) / ctas) > RING_BYTES || (c.N * ctas * 2 <= sms && pieces > 2 * ctas * 2 * RTH))) ctas *= 2;
+        const int per = (pieces + ctas - 1) / ctas, bufs = (int)std::min<long long>(RING, RING_BYTES / (16ll * per));
+        if (bufs < 1) return PL_ERR_INVALID;
+        auto kernel = ring_kernel<T>;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES) != cudaSuccess) return launched();
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3(rows * ctas);
-        cfg.blockDim = dim3(STH);
+        cfg.gridDim = dim3((unsigned)(std::min(c.N, std::max(1ll, 2 * sms / ctas)) * ctas));
+        cfg.blockDim = dim3(RTH);
+        cfg.dynamicSmemBytes = (size_t)bufs * per * 16;
         cfg.stream = stream;
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim = {(unsigned)ctas, 1, 1};
         cfg.attrs = at;
         cfg.numAttrs = 1;
-        cudaLaunchKernelEx(&cfg, stream_kernel<T>, c, ctas);
+        cudaLaunchKernelEx(&cfg, kernel, c, ctas, per, bufs);
     }
     return launched();
 }

@@ -69,7 +69,7 @@ def test_policy_loss_arguments(pkg):
     def call(z=FAKE, type=0, N=4, V=7, stride=7, a=FAKE, old=FAKE, adv=FAKE, lo=0.2, hi=0.2, kl=0.0, loss=FAKE, logp=FAKE, dz=FAKE, ds=7):
         return lib.policy_loss(z, type, N, V, stride, a, old, adv, None, None, lo, hi, kl, loss, logp, dz, ds, None)
     nan, inf = float("nan"), float("inf")
-    for bad in (dict(z=None), dict(type=2), dict(N=-1), dict(V=0), dict(V=(1 << 24) + 1, stride=1 << 25, ds=1 << 25), dict(stride=6), dict(ds=6), dict(a=None),
+    for bad in (dict(z=None), dict(type=2), dict(N=-1), dict(V=0), dict(V=200001, stride=1 << 25, ds=1 << 25), dict(stride=6), dict(ds=6), dict(a=None),
                 dict(old=None), dict(adv=None), dict(loss=None), dict(logp=None), dict(z=FAKE + 2), dict(dz=FAKE + 1), dict(lo=-0.1), dict(hi=-0.1), dict(lo=nan),
                 dict(hi=inf), dict(kl=nan), dict(ds=9), dict(N=1 << 29)):
         assert call(**bad) == pl.PL_ERR_INVALID, bad
