@@ -4,15 +4,16 @@
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+from array import array
+from itertools import chain, repeat
 from operator import attrgetter
 from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
 
-from .binding import JsError, JS_ERR_ARG, load_library, _stream_ptr
+from .binding import JsError, JS_ERR_ARG, load_library, _elsewhere, _stream_ptr, _there
 
 ADAMW_OK, ADAMW_ERR_INVALID, ADAMW_ERR_CUDA = 0, -1, -2
 ADAMW_BLOCK = 256
@@ -122,7 +123,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     if copies is not None:
         _same(copies, torch.bfloat16, index, sizes, "copies")
     bits = 32 if m.dtype is f32 else 8
-    stype, places = (f32 if bits == 32 else torch.float8_e4m3fn), _places(sizes)
+    counts = np.frombuffer(array("q", sizes), dtype=np.int64)
+    stype, places = (f32 if bits == 32 else torch.float8_e4m3fn), int(((counts + (ADAMW_BLOCK - 1)) // ADAMW_BLOCK).sum()) * ADAMW_BLOCK
     for t, what in ((m, "m"), (v, "v")):
         if not (t.dtype is stype and t.get_device() == index and t.is_contiguous() and t.numel() == places):
             _bad(f"state.{what}: expected {places} contiguous values of {stype} on the parameters' device")
@@ -133,10 +135,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     live = pointers if 0 not in sizes else [a for a, k in zip(pointers, sizes) if k]
     if len(set(live)) != len(live):
         _bad("params: the same tensor twice")
-    table = np.empty((4, n), dtype=np.int64)
-    table[0], table[1], table[3] = pointers, list(map(_data_ptr, grads)), sizes
-    table[2] = 0 if copies is None else list(map(_data_ptr, copies))
-    table = np.ascontiguousarray(table.T)
+    # the header's table of tensors: parameter, gradient, copy, size
+    table = array("q", chain.from_iterable(zip(pointers, map(_data_ptr, grads), repeat(0) if copies is None else map(_data_ptr, copies), sizes)))
     o = _Options(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=-1 if seed is None else int(seed) & 0xFFFFFFFF)
     if isinstance(step, torch.Tensor):
         o.step_dev = _one(step, torch.int64, device, "step")
@@ -148,20 +148,12 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
         o.lr = float(lr)
     o.grad_scale = _one(grad_scale, f32, device, "grad_scale")
     o.skip = _one(skip, torch.int32, device, "skip")
-    with _on(device):
-        rc = _lib().adamw_step(table.ctypes.data, n, 0 if gtype is f32 else 1, bits, m.data_ptr(), v.data_ptr(),
-                               m_scale.data_ptr() if bits == 8 else None, v_scale.data_ptr() if bits == 8 else None, C.byref(o), _stream_ptr(stream))
+    args = (table.buffer_info()[0], n, 0 if gtype is f32 else 1, bits, m.data_ptr(), v.data_ptr(), m_scale.data_ptr() if bits == 8 else None,
+            v_scale.data_ptr() if bits == 8 else None, C.byref(o))
+    if _elsewhere(index, stream):
+        with _there(index, stream):
+            rc = _lib().adamw_step(*args, _stream_ptr(None))
+    else:
+        rc = _lib().adamw_step(*args, _stream_ptr(None))
     if rc != ADAMW_OK:
         raise JsError(rc, "adamw_step: " + (_lib().adamw_last_error().decode() if rc == ADAMW_ERR_CUDA else "argument outside the documented limits"))
-
-
-def _on(device):
-    """The tensors' device as the current one, for the call."""
-    if device.index == torch._C._cuda_getDevice():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
-
-
-def _stream(stream):
-    """New tensors belong to the stream that the call runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)

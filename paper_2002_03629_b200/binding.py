@@ -2,6 +2,7 @@
 marshalling only.  Fails loudly if the library is missing; there is no fallback."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -107,6 +108,18 @@ def _stream_ptr(stream) -> Optional[int]:
     if stream is None:       # the current stream's handle without building a Stream object (3.4 us)
         return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return C.c_void_p(stream.cuda_stream)
+
+
+def _elsewhere(index: int, stream) -> bool:
+    """Does a call on tensors of this device run on another device or stream than the current one?"""
+    return stream is not None or index != torch._C._cuda_getDevice()
+
+
+@contextlib.contextmanager
+def _there(index: int, stream):
+    """The tensors' device and the call's stream as the current ones (new tensors belong to that stream)."""
+    with torch.cuda.device(index), torch.cuda.stream(stream):
+        yield
 
 
 def _dev(t: Optional[torch.Tensor], dtype, what: str):
