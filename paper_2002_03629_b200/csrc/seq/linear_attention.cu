@@ -18,19 +18,66 @@ int status(cudaError_t e)
 }
 
 // ------------------------------------------------------------------ any type, size and stride
-// A CTA carries VS columns of the state of one sequence and head through chunks of CH steps, all in fp32 by multiply-adds:
+// A CTA carries VS columns of the state of one sequence and head through chunks of CH steps, all in fp32 by multiply-adds, sums in a fixed order:
 //     A = (q k^T) * lambda^(i-j), j <= i;     o = A v + lambda^(i+1) q S;     S = lambda^CH S + sum_j lambda^(CH-1-j) k_j v_j^T
-constexpr int CH = 32, VS = 32, GTH = 256, QP = LA_MAX_D + 1, AP = CH + 1, VP = VS + 1;
-constexpr size_t G_SMEM = (size_t)(2 * CH * QP + CH * VP + CH * AP + LA_MAX_D * VP + CH + 1) * sizeof(float);
+// Bound: the multiply-adds and the shared-memory loads that feed them: tiles of outputs in registers (4 x 4, for the state 4 x 4 to 8 x 8, which
+// stays there), operands in shared memory with the summed index in rows, so that a thread reads its four or eight values in one or two loads.  The next
+// chunk's rows are on their way from memory while this one is computed.  Chunks of 32 steps: twice as long the products of scores would outweigh the
+// others at the widths this path is used for.
+constexpr int CH = 32;
 
-template <typename T>
-__global__ void __launch_bounds__(GTH) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
+template <int DK, int VS, int G>
+struct AnyTiles {
+    static constexpr int QS = CH + 4;                       // row of q^T, k^T, A^T
+    static constexpr int SR = VS * DK / G / 4 > 8 ? 8 : 4, SC = DK * VS / G / SR;      // the state's tile: rows (Dk) x columns
+    static constexpr int OC = 4, OR = CH * VS / G / OC;     // the output's
+    static constexpr int AC = 4, AR = CH * CH / G / AC;     // the scores'
+    static constexpr int KW = DK + 4, VW = VS + 4;
+    static constexpr int FLOATS = 2 * DK * QS + CH * KW + CH * VW + CH * QS + DK * VW + 2 * CH + 2;
+    static_assert(SC % 4 == 0 && OR >= 1 && AR >= 1, "four columns a load");
+};
+
+// N neighbouring values of shared memory, on 16 bytes for N >= 4
+template <int N>
+__device__ __forceinline__ void take(const float *p, float (&x)[N])
 {
-    extern __shared__ float sm[];
+    if constexpr (N == 1) x[0] = *p;
+    else if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        x[0] = v.x; x[1] = v.y;
+    } else
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(p + e);
+            x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
+        }
+}
+// acc[r][c] += sum over k of a[k][r0 + r] b[k][c0 + c]; rows of a and b `sa` and `sb` apart
+template <int R, int N>
+__device__ __forceinline__ void multiply(float (&acc)[R][N], const float *a, int sa, const float *b, int sb, int steps)
+{
+#pragma unroll 4
+    for (int k = 0; k < steps; ++k) {
+        float x[R], y[N];
+        take<R>(a + k * sa, x);
+        take<N>(b + k * sb, y);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < N; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+    }
+}
+
+template <typename T, int DK, int VS, int G>
+__global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
+{
+    using L = AnyTiles<DK, VS, G>;
+    extern __shared__ __align__(16) float sm[];
     const LaJob &job = jobs.job[blockIdx.z];
     const int Dk = job.Dk, c0 = blockIdx.y * VS, tid = threadIdx.x;
     if (c0 >= job.Dv) return;
-    float *const q = sm, *const k = q + CH * QP, *const v = k + CH * QP, *const A = v + CH * VP, *const S = A + CH * AP, *const pw = S + LA_MAX_D * VP;
+    float *const qt = sm, *const kt = qt + DK * L::QS, *const kw = kt + DK * L::QS, *const v = kw + CH * L::KW, *const At = v + CH * L::VW, *const S = At + CH * L::QS,
+          *const pw = S + DK * L::VW;                        // pw[n] = lambda^n, n <= CH
     const int cols = min(VS, job.Dv - c0), seq = blockIdx.x / seqs.H, h = blockIdx.x % seqs.H;
     long long start;
     const int n = la_sequence(seqs, seq, start);
@@ -41,72 +88,103 @@ __global__ void __launch_bounds__(GTH) la_any_kernel(const __grid_constant__ LaJ
     const T *const vg = (const T *)job.v.data + b * job.v.batch + start * job.v.token + h * job.v.head + c0;
     T *const og = (T *)job.o.data + b * job.o.batch + start * job.o.token + h * job.o.head + c0;
     const size_t sbase = (size_t)blockIdx.x * Dk * job.Dv;
-    for (int p = tid; p <= CH; p += GTH) pw[p] = la_power(ld, p);
-    for (int p = tid; p < Dk * VS; p += GTH) {
-        const int d = p / VS, c = p % VS;
-        S[d * VP + c] = job.s0 != nullptr && c < cols ? job.s0[sbase + (job.turned ? (size_t)(c0 + c) * Dk + d : (size_t)d * job.Dv + c0 + c)] : 0.0f;
-    }
+    for (int p = tid; p <= CH; p += G) pw[p] = la_power(ld, p);
+    // this thread's tiles: state, output, scores
+    const int sr = tid / (VS / L::SC) * L::SR, sc = tid % (VS / L::SC) * L::SC;
+    const int orow = tid / (VS / L::OC) * L::OR, oc = tid % (VS / L::OC) * L::OC;
+    const int ar = tid / (CH / L::AC) * L::AR, ac = tid % (CH / L::AC) * L::AC;
+    float St[L::SR][L::SC];
+#pragma unroll
+    for (int r = 0; r < L::SR; ++r)
+#pragma unroll
+        for (int c = 0; c < L::SC; ++c) {
+            const int d = sr + r, e = sc + c;
+            St[r][c] = job.s0 != nullptr && d < Dk && e < cols
+                           ? job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)] : 0.0f;
+        }
+    // a chunk's rows, by way of registers: thread = a column and every (G / width)-th step
+    constexpr int NQ = CH * DK / G, NV = CH * VS / G, RQ = G / DK, RV = G / VS;
+    const int qi = tid / DK, qd = tid % DK, vi = tid / VS, vc = tid % VS;
+    float rq[NQ], rk[NQ], rv[NV];
+    auto fetch = [&](int t0) {
+        const long long sign = job.back ? -1 : 1, t = job.back ? n - 1 - t0 : t0;
+        const T *pq = qg + (t + sign * qi) * job.q.token + qd, *pk = kg + (t + sign * qi) * job.k.token + qd, *pv = vg + (t + sign * vi) * job.v.token + vc;
+        const long long sq = sign * RQ * job.q.token, sk = sign * RQ * job.k.token, sv = sign * RV * job.v.token;
+#pragma unroll
+        for (int p = 0; p < NQ; ++p, pq += sq, pk += sk) {
+            const bool in = t0 + qi + p * RQ < n && qd < Dk;
+            rq[p] = in ? la_value(pq) : 0.0f;
+            rk[p] = in ? la_value(pk) : 0.0f;
+        }
+#pragma unroll
+        for (int p = 0; p < NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_value(pv) : 0.0f;
+    };
+    if (n > 0) fetch(0);
     int late = job.back ? 0 : 1;
+#pragma unroll 1
     for (int t0 = 0; t0 < n; t0 += CH, late = 1) {
         const int rows = min(CH, n - t0);
-        __syncthreads();
-        for (int p = tid; p < CH * Dk; p += GTH) {
-            const int i = p / Dk, d = p % Dk;
-            const long long t = job.back ? n - 1 - t0 - i : t0 + i;
-            q[i * QP + d] = i < rows ? la_value(qg + t * job.q.token + d) : 0.0f;
-            k[i * QP + d] = i < rows ? la_value(kg + t * job.k.token + d) : 0.0f;
-        }
-        for (int p = tid; p < CH * VS; p += GTH) {
-            const int i = p / VS, c = p % VS;
-            const long long t = job.back ? n - 1 - t0 - i : t0 + i;
-            v[i * VP + c] = i < rows && c < cols ? la_value(vg + t * job.v.token + c) : 0.0f;
-        }
-        __syncthreads();
-        const int i = tid / 8;
+        __syncthreads();                                     // the chunk before is done with
 #pragma unroll
-        for (int m = 0; m < CH / 8; ++m) {
-            const int j = tid % 8 + 8 * m;
-            float a = 0.0f;
-            if (j <= i && i < rows) {
-                for (int d = 0; d < Dk; ++d) a = fmaf(q[i * QP + d], k[j * QP + d], a);
-                a *= pw[i - j] * job.sum_scale;
+        for (int p = 0; p < NQ; ++p) {
+            const int i = qi + p * RQ;
+            qt[qd * L::QS + i] = rq[p];
+            kt[qd * L::QS + i] = rk[p];
+            kw[i * L::KW + qd] = i < rows ? rk[p] * (job.sum_scale * pw[rows - 1 - i]) : 0.0f;
+        }
+#pragma unroll
+        for (int p = 0; p < NV; ++p) {
+            v[(vi + p * RV) * L::VW + vc] = rv[p];
+        }
+#pragma unroll
+        for (int r = 0; r < L::SR; ++r)
+#pragma unroll
+            for (int c = 0; c < L::SC; c += 4) *reinterpret_cast<float4 *>(S + (sr + r) * L::VW + sc + c) = make_float4(St[r][c], St[r][c + 1], St[r][c + 2], St[r][c + 3]);
+        __syncthreads();
+        if (t0 + CH < n) fetch(t0 + CH);
+        {
+            float acc[L::AR][L::AC] = {};
+            if (ar + L::AR > ac) multiply<L::AR, L::AC>(acc, qt + ar, L::QS, kt + ac, L::QS, DK);          // (above the diagonal there is nothing)
+#pragma unroll
+            for (int r = 0; r < L::AR; ++r)
+#pragma unroll
+                for (int c = 0; c < L::AC; ++c) {
+                    const int i = ar + r, j = ac + c;
+                    At[j * L::QS + i] = j <= i && i < rows ? acc[r][c] * (job.sum_scale * pw[i - j]) : 0.0f;
+                }
+        }
+        __syncthreads();
+        {
+            float from[L::OR][L::OC] = {}, own[L::OR][L::OC] = {};
+            multiply<L::OR, L::OC>(from, qt + orow, L::QS, S + oc, L::VW, DK);
+            multiply<L::OR, L::OC>(own, At + orow, L::QS, v + oc, L::VW, orow + L::OR);
+#pragma unroll
+            for (int r = 0; r < L::OR; ++r) {
+                const int i = orow + r;
+                if (i >= rows) continue;
+                const long long t = job.back ? n - 1 - t0 - i : t0 + i;
+                T *const to = og + t * job.o.token + oc;
+                const float f = pw[i + late];
+#pragma unroll
+                for (int c = 0; c < L::OC; ++c)
+                    if (oc + c < cols) la_put(to + c, job.out_scale * fmaf(f, from[r][c], own[r][c]));
             }
-            A[i * AP + j] = a;
         }
-        __syncthreads();
-        if (i < rows) {
-            const long long t = job.back ? n - 1 - t0 - i : t0 + i;
-            float o[VS / 8], f[VS / 8];
-#pragma unroll
-            for (int m = 0; m < VS / 8; ++m) { o[m] = 0.0f; f[m] = 0.0f; }
-            for (int j = 0; j <= i; ++j)
-#pragma unroll
-                for (int m = 0; m < VS / 8; ++m) o[m] = fmaf(A[i * AP + j], v[j * VP + tid % 8 + 8 * m], o[m]);
-            for (int d = 0; d < Dk; ++d)
-#pragma unroll
-                for (int m = 0; m < VS / 8; ++m) f[m] = fmaf(q[i * QP + d], S[d * VP + tid % 8 + 8 * m], f[m]);
-#pragma unroll
-            for (int m = 0; m < VS / 8; ++m) {
-                const int c = tid % 8 + 8 * m;
-                if (c < cols) la_put(og + t * job.o.token + c, job.out_scale * fmaf(pw[i + late], f[m], o[m]));
-            }
-        }
-        __syncthreads();
         const LaStep step(ld, rows - 1 + late);
-        for (int p = tid; p < Dk * VS; p += GTH) {
-            const int d = p / VS, c = p % VS;
-            float u = 0.0f;
-            for (int j = 0; j < rows; ++j) u = fmaf(pw[rows - 1 - j] * k[j * QP + d], v[j * VP + c], u);
-            S[d * VP + c] = step(S[d * VP + c], job.sum_scale * u);
-        }
+        float U[L::SR][L::SC] = {};
+        multiply<L::SR, L::SC>(U, kw + sr, L::KW, v + sc, L::VW, CH);
+#pragma unroll
+        for (int r = 0; r < L::SR; ++r)
+#pragma unroll
+            for (int c = 0; c < L::SC; ++c) St[r][c] = step(St[r][c], U[r][c]);
     }
-    __syncthreads();
     if (job.s1 == nullptr) return;
     const float last = job.back && n > 0 ? la_power(ld, 1) : 1.0f;
-    for (int p = tid; p < Dk * VS; p += GTH) {
-        const int d = p / VS, c = p % VS;
-        if (c < cols) job.s1[sbase + (size_t)d * job.Dv + c0 + c] = last * S[d * VP + c];
-    }
+#pragma unroll
+    for (int r = 0; r < L::SR; ++r)
+#pragma unroll
+        for (int c = 0; c < L::SC; ++c)
+            if (sr + r < Dk && sc + c < cols) job.s1[sbase + (size_t)(sr + r) * job.Dv + c0 + sc + c] = last * St[r][c];
 }
 
 // ------------------------------------------------------------------ single steps
@@ -191,6 +269,27 @@ bool tensor_ok(const la_shape *s, const la_tensor *t, long long rows)
     return t->data != nullptr && (reinterpret_cast<uintptr_t>(t->data) & (s->type == LA_F32 ? 3u : 1u)) == 0;
 }
 
+template <typename T, int DK, int VS, int G>
+cudaError_t launch_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dv, cudaStream_t stream)
+{
+    auto kernel = la_any_kernel<T, DK, VS, G>;
+    constexpr size_t smem = AnyTiles<DK, VS, G>::FLOATS * sizeof(float);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<dim3((unsigned)(seqs.n * seqs.H), (dv + VS - 1) / VS, count), G, smem, stream>>>(jobs, seqs);
+    return cudaGetLastError();
+}
+// Widths up to 32, 64, 128; at 128 the state's columns are shared by two CTAs, each of which computes the scores
+template <typename T>
+cudaError_t run_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dk, int dv, cudaStream_t stream)
+{
+    if (dk <= 32) return launch_any<T, 32, 32, 64>(jobs, seqs, count, dv, stream);
+    // (few of them: halves of the state's columns, one prompt of 100 steps, 8 heads of 64: 29 -> 21 us)
+    const bool few = (long long)seqs.n * seqs.H * count * 2 <= 148;
+    if (dk <= 64) return dv <= 32 || few ? launch_any<T, 64, 32, 128>(jobs, seqs, count, dv, stream) : launch_any<T, 64, 64, 128>(jobs, seqs, count, dv, stream);
+    return launch_any<T, 128, 64, 256>(jobs, seqs, count, dv, stream);
+}
+
 int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const *tensors, int n_in, int n_all, const int (*which)[3], void *workspace,
         cudaStream_t stream)
 {
@@ -200,12 +299,12 @@ int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const
     for (int j = 0; j < count; ++j)
         aligned = aligned && ((reinterpret_cast<uintptr_t>(jobs.job[j].s0) | reinterpret_cast<uintptr_t>(jobs.job[j].s1)) & 15u) == 0;
     if (aligned && la_tc_takes(s, count, tensors, n_all)) return status(la_tc_run(s, jobs, count, tensors, n_in, which, workspace, stream));
-    int dv = 0;
-    for (int j = 0; j < count; ++j) dv = std::max(dv, jobs.job[j].Dv);
-    auto kernel = s->type == LA_F32 ? la_any_kernel<float> : la_any_kernel<__nv_bfloat16>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G_SMEM) != cudaSuccess) return status(cudaGetLastError());
-    kernel<<<dim3((unsigned)(seqs.n * s->H), (dv + VS - 1) / VS, count), GTH, G_SMEM, stream>>>(jobs, seqs);
-    return status(cudaGetLastError());
+    int dk = 0, dv = 0;
+    for (int j = 0; j < count; ++j) {
+        dk = std::max(dk, jobs.job[j].Dk);
+        dv = std::max(dv, jobs.job[j].Dv);
+    }
+    return status(s->type == LA_F32 ? run_any<float>(jobs, seqs, count, dk, dv, stream) : run_any<__nv_bfloat16>(jobs, seqs, count, dk, dv, stream));
 }
 
 }  // namespace

@@ -114,6 +114,16 @@ def test_backward(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(45, 37, 2, 64, 64), (40, 33, 2, 47, 50), (160, 3, 1, 30, 32), (80, 40, 1, 128, 65)], ids=str)
+def test_many_sequences(size, dtype):
+    """Enough of them that no head's columns are split to fill the GPU."""
+    x = make(*size, dtype, seed=2)
+    o, S = forward(x, 0.2)
+    check_forward(x, o, S, 0.2)
+    check_backward(x, backward(x, 0.2), 0.2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("decays", [[0.0, -30.0], [-1e-6, -100.0], [float("-inf"), -2e-4]], ids=str)
 def test_decays_from_none_to_everything(decays, dtype):
     x = make(1, 270, 2, 64, 64, dtype, decays=decays)
