@@ -8,7 +8,7 @@
 struct LaPlan {
     int seg, slots;
     bool fits;                               // in 31 bits
-    size_t bytes;                            // of workspace: the segments' states
+    size_t order, bytes;                     // workspace: the segments' states, from byte `order` on the order of packed sequences' segments, and all of it
 };
 LaPlan la_tc_plan(const la_shape *s, int jobs);
 // May these tensors take the path?  `tensors`: the inputs first, then what is written

@@ -39,6 +39,10 @@ struct Params {
     int seg;                                 // steps of a segment, a multiple of C
     int units;
     float *carry;                            // [job][slot][head][Dk][Dv]
+    // packed sequences: the next unit to be taken, the number of segments, how many have others behind them; the segments (sequence, number in
+    // it), longest first, those with others behind them before all
+    int *next;
+    int2 *order;
 };
 
 struct Unit {
@@ -48,37 +52,38 @@ struct Unit {
     long long start;
 };
 
-// Unit u, or false: none.  With cu_seqlens, sequence s owns the slots from cu[s] / seg + s on, at least as many as it has segments.
-__device__ __forceinline__ bool get_unit(const Params &p, int u, Unit &x)
+// The slot of a packed sequence's first segment: it owns at least as many as it has segments
+__device__ __forceinline__ int first_slot(const LaSeqs &seqs, int seg, int seq) { return min(max(__ldg(seqs.cu + seq), 0), (int)seqs.T) / seg + seq; }
+// How many units there are (packed sequences: known to the device only)
+__device__ __forceinline__ int unit_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.next + 1) * p.seqs.H * p.jobs; }
+
+// ... and how many may be of segments with others behind them
+__device__ __forceinline__ int cut_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.next + 2) * p.seqs.H * p.jobs; }
+
+// Unit u
+__device__ __forceinline__ void get_unit(const Params &p, int u, Unit &x)
 {
     x.job = u % p.jobs;
     u /= p.jobs;
     x.h = u % p.seqs.H;
-    x.slot = u / p.seqs.H;
+    u /= p.seqs.H;
     int s;
     if (p.seqs.cu == nullptr) {
-        x.seq = x.slot / p.per;
-        s = x.slot % p.per;
+        x.slot = u;
+        x.seq = u / p.per;
+        s = u % p.per;
     } else {
-        int lo = 0, hi = p.seqs.n;
-        auto first = [&](int q) { return min(max(__ldg(p.seqs.cu + q), 0), (int)p.seqs.T) / p.seg + q; };
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first(mid) <= x.slot) lo = mid;
-            else hi = mid;
-        }
-        x.seq = lo;
-        s = x.slot - first(lo);
-        if (s < 0) return false;
+        const int2 e = __ldg(p.order + u);
+        x.seq = e.x;
+        s = e.y;
+        x.slot = first_slot(p.seqs, p.seg, x.seq) + s;
     }
     x.n = la_sequence(p.seqs, x.seq, x.start);
     const long long at = (long long)s * p.seg;
-    if (s > 0 && at >= x.n) return false;
     const long long end = min(at + p.seg, (long long)x.n);
     x.c0 = (int)(at / C);
     x.c1 = (int)((end + C - 1) / C);
     x.last = end == x.n;
-    return true;
 }
 
 // Where the last state is asked for, a chunk's sum reaches it with the weight lambda^(steps behind the chunk).  Two pieces of K leave the sum off by
@@ -405,11 +410,12 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             if (++slot == RING) { slot = 0; heard_par ^= 1u; }
         };
         Work w{};
+        const int units = unit_count(p);
 #pragma unroll 1
-        for (int u = blockIdx.x; u <= p.units + (int)gridDim.x && on; u += gridDim.x) {
+        for (int u = blockIdx.x; on;) {
             Unit x{};
-            const bool end = u >= p.units;
-            if (!end && !get_unit(p, u, x)) continue;
+            const bool end = u >= units;
+            if (!end) get_unit(p, u, x);
             const LaJob &job = p.job[x.job];
             const size_t size = (size_t)job.Dk * job.Dv, state = ((size_t)x.seq * p.seqs.H + x.h) * size;
             w.n = x.n; w.c0 = x.c0; w.c1 = x.c1;
@@ -453,6 +459,9 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                 ++loads;
                 if (++stage == L::STAGES) { stage = 0; par ^= 1u; }
             }
+            // Units of one length: every gridDim-th; of different ones: the next that nobody has
+            if (p.seqs.cu == nullptr) u += gridDim.x;
+            else u = __shfl_sync(0xffffffffu, lane == 0 ? atomicAdd(p.next, 1) : 0, 0);
         }
         // the last outputs, oldest first
         if (loads < L::STAGES) stage = 0;                                          // (par is then that of no load: the first of `staged` is due)
@@ -890,9 +899,11 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
         ++g;
     };
     // (after a wait that gave up the S role goes on alone and writes NaN)
-    for (int u = blockIdx.x; u < p.units && (on || (warp >> 2) == 1); u += gridDim.x) {
+    const int units = cut_count(p);
+    for (int u = blockIdx.x; u < units && (on || (warp >> 2) == 1); u += gridDim.x) {
         Unit x;
-        if (!get_unit(p, u, x) || x.last) continue;
+        get_unit(p, u, x);
+        if (x.last) continue;
         const LaJob &job = p.job[x.job];
         const bool back = job.back != 0;
         const float ld = p.seqs.log_decay[x.h];
@@ -1015,34 +1026,88 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
 
 // They become the states that the segments start from: C_0 = S0, C_{i+1} = lambda^seg C_i + own_i.  A thread per value; the loads do not wait for
 // the sums (eight segments' worth in flight).
-__global__ void la_carry_kernel(LaJobs jobs, LaSeqs seqs, int slots, int per, int seg, float *carry)
+__global__ void la_carry_kernel(LaJobs jobs, LaSeqs seqs, int slots, int per, int seg, const int *next, const int2 *order, float *carry)
 {
-    const int job_i = blockIdx.z, h = blockIdx.x % seqs.H, seq = blockIdx.x / seqs.H;
+    const int job_i = blockIdx.z, h = blockIdx.x % seqs.H;
+    int seq = blockIdx.x / seqs.H;
     const LaJob &job = jobs.job[job_i];
     const int e = blockIdx.y * blockDim.x + threadIdx.x, size = job.Dk * job.Dv;
+    if (seqs.cu != nullptr) {                                // only sequences that are cut
+        if (seq >= next[2]) return;
+        const int2 s = order[seq];
+        if (s.y != 0) return;
+        seq = s.x;
+    }
     if (e >= size) return;
     long long start;
     const int n = la_sequence(seqs, seq, start);
-    const int slot = seqs.cu == nullptr ? seq * per : min(max(seqs.cu[seq], 0), (int)seqs.T) / seg + seq;
+    const int slot = seqs.cu == nullptr ? seq * per : first_slot(seqs, seg, seq);
     const int d = e / job.Dv, v = e % job.Dv, parts = (n + seg - 1) / seg;
     float S = 0.0f;
     if (job.s0 != nullptr) S = job.s0[((size_t)seq * seqs.H + h) * size + (job.turned ? (size_t)v * job.Dk + d : (size_t)e)];
     const float ld = seqs.log_decay[h];
     const LaStep step(ld, seg);
     float *c = carry + (((size_t)job_i * slots + slot) * seqs.H + h) * size + e;
-    const size_t next = (size_t)seqs.H * size;
+    const size_t step_on = (size_t)seqs.H * size;
     if (parts > 1) S = LaStep(ld, seg - (job.back ? 1 : 0))(S, *c);       // (the first segment starts from S0 itself)
-    c += next;
-    for (int i0 = 1; i0 < parts; i0 += 8, c += 8 * next) {
+    c += step_on;
+    for (int i0 = 1; i0 < parts; i0 += 8, c += 8 * step_on) {
         float own[8];                                        // the last segment's own state is not there, nor wanted
 #pragma unroll
-        for (int i = 0; i < 8; ++i) own[i] = i0 + i + 1 < parts ? c[i * next] : 0.0f;
+        for (int i = 0; i < 8; ++i) own[i] = i0 + i + 1 < parts ? c[i * step_on] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i0 + i < parts) {
-                c[i * next] = S;
+                c[i * step_on] = S;
                 S = step(S, own[i]);
             }
+    }
+}
+
+// Packed sequences: their segments, sorted by length in 256 steps (the order among equals changes nothing but who works on what), and the counter that the
+// units are taken by, `grid` of them gone.  One CTA: there are few segments beyond a sequence's first.
+constexpr int ORDER_TH = 1024, BINS = 256;
+__global__ void __launch_bounds__(ORDER_TH) la_order_kernel(LaSeqs seqs, int seg, int slots, int grid, int *next, int2 *order)
+{
+    __shared__ int bin[BINS], total, cut;
+    const int tid = threadIdx.x;
+    for (int i = tid; i < BINS; i += ORDER_TH) bin[i] = 0;
+    __syncthreads();
+    auto each = [&](auto &&f) {
+        for (int q = tid; q < seqs.n; q += ORDER_TH) {
+            long long start;
+            const int n = la_sequence(seqs, q, start), full = n > 0 ? (n - 1) / seg : 0;       // (all but the last one are whole)
+            for (int s = 0; s <= full; ++s)
+                f(q, s, s < full ? 0 : BINS - 1 - (int)((long long)((n - full * seg + C - 1) / C) * (BINS - 2) / (seg / C)));
+        }
+    };
+    each([&](int, int, int b) { atomicAdd(&bin[b], 1); });
+    __syncthreads();
+    if (tid < 32) {
+        int own[BINS / 32], sum = 0;
+        for (int i = 0; i < BINS / 32; ++i) {
+            own[i] = sum;
+            sum += bin[tid * (BINS / 32) + i];
+        }
+        int before = sum;
+        for (int d = 1; d < 32; d *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, before, d);
+            if (tid >= d) before += x;
+        }
+        if (tid == 31) total = before;
+        if (tid == 0) cut = bin[0];
+        before -= sum;
+        for (int i = 0; i < BINS / 32; ++i) bin[tid * (BINS / 32) + i] = before + own[i];
+    }
+    __syncthreads();
+    each([&](int q, int s, int b) {
+        const int at = atomicAdd(&bin[b], 1);
+        if (at < slots) order[at] = make_int2(q, s);         // (more segments than slots: offsets that go back)
+    });
+    if (tid == 0) {
+        next[0] = grid;
+        next[1] = min(total, slots);
+        next[2] = min(cut, slots);
     }
 }
 
@@ -1082,12 +1147,15 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
         const long long per = (chunks + parts - 1) / parts, c = (heads * parts + sms - 1) / sms * (per + 1) * 8 / 5 + 6;
         if (c < cost) { cost = c; best = per; }
     }
+    // Packed sequences: their lengths are the device's.  None of more than twice what an SM has to do, so that no long one holds up the end
+    if (s->cu_seqlens != nullptr && n > 1) best = std::min(best, std::max(8ll, 2 * ((s->T / C + n) * s->H * jobs / sms + 1)));
     LaPlan plan;
     plan.seg = (int)std::min(best * C, 1ll << 30);
     const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
     plan.fits = slots * s->H * jobs < (1ll << 30) && s->T < (1ll << 30);
     plan.slots = plan.fits ? (int)slots : 0;
-    plan.bytes = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
+    plan.order = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
+    plan.bytes = plan.order + (plan.fits && s->cu_seqlens != nullptr ? 8 * ((size_t)slots + 2) : 0);
     return plan;
 }
 
@@ -1142,10 +1210,19 @@ cudaError_t la_tc_run(const la_shape *s, const LaJobs &jobs, int count, const la
     p.carry = (float *)workspace;
     p.units = plan.slots * s->H * count;
     const int sms = sm_count();
+    if (s->cu_seqlens != nullptr) {
+        p.next = reinterpret_cast<int *>((char *)workspace + plan.order);
+        p.order = reinterpret_cast<int2 *>(p.next + 4);
+        la_order_kernel<<<1, ORDER_TH, 0, stream>>>(p.seqs, p.seg, p.slots, std::min(p.units, sms), p.next, p.order);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
     if (plan.slots > n) {
         cudaError_t e = launch(p, dk, dv, true, sms, stream);
         if (e != cudaSuccess) return e;
-        la_carry_kernel<<<dim3((unsigned)(n * s->H), (unsigned)((s->Dk * s->Dv + 255) / 256), (unsigned)count), 256, 0, stream>>>(jobs, p.seqs, p.slots, p.per, p.seg, p.carry);
+        const int cut = s->cu_seqlens != nullptr ? plan.slots - n : n;             // sequences that may be
+        la_carry_kernel<<<dim3((unsigned)(cut * s->H), (unsigned)((s->Dk * s->Dv + 255) / 256), (unsigned)count), 256, 0, stream>>>(jobs, p.seqs, p.slots, p.per,
+                                                                                                                            p.seg, p.next, p.order, p.carry);
         e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }

@@ -150,7 +150,7 @@ def test_whole_numbers_are_exact_on_the_tensor_cores():
                 assert torch.equal(got.cpu(), torch.from_numpy(want).to(got.dtype))
 
 
-LENS = [[1, 130, 0, 64, 257, 5], [0, 0, 3], [128, 128], [1] * 40, [500]]
+LENS = [[1, 130, 0, 64, 257, 5], [0, 0, 3], [128, 128], [1] * 40, [500], [2600, 1, 1024, 1025, 0, 130, 2048], [17] * 100 + [700]]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
@@ -190,6 +190,14 @@ def test_offsets_outside_the_rows_touch_nothing_else():
     o, S = la.linear_attention(d["q"], d["k"], d["v"], d["ld"], cu_seqlens=cu, out=whole[1:2])
     torch.cuda.synchronize()
     assert (whole[0] == 9).all() and (whole[2] == 9).all() and torch.isfinite(S).all() and (S[1] == 0).all()
+    # rows that many sequences claim, more of them than there is room for segments of
+    x = make(1, 3000, 1, 32, 32, torch.bfloat16, state=False)
+    d, whole = dev(x), torch.full((3, 3000, 1, 32), 9.0, dtype=torch.bfloat16, device="cuda")
+    cu = torch.tensor([0, 3000] * 60, dtype=torch.int32).cuda()
+    la.linear_attention(d["q"], d["k"], d["v"], d["ld"], cu_seqlens=cu, out=whole[1:2])
+    la.linear_attention_backward(d["q"], d["k"], d["v"], d["ld"], d["do"], cu_seqlens=cu)
+    torch.cuda.synchronize()
+    assert (whole[0] == 9).all() and (whole[2] == 9).all()
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
