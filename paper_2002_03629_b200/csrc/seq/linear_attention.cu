@@ -31,7 +31,7 @@ struct AnyTiles {
     static constexpr int QS = CH + 4;                       // row of q^T, k^T, A^T
     static constexpr int SR = VS * DK / G / 4 > 8 ? 8 : 4, SC = DK * VS / G / SR;      // the state's tile: rows (Dk) x columns
     static constexpr int OC = 4, OR = CH * VS / G / OC;     // the output's
-    static constexpr int AC = 4, AR = CH * CH / G / AC;     // the scores'
+    static constexpr int AC = 4, AR = CH * CH / G / AC;     // the scores', neighbours along i
     static constexpr int KW = DK + 4, VW = VS + 4;
     static constexpr int FLOATS = 2 * DK * QS + CH * KW + CH * VW + CH * QS + DK * VW + 2 * CH + 2;
     static_assert(SC % 4 == 0 && OR >= 1 && AR >= 1, "four columns a load");
@@ -51,6 +51,19 @@ __device__ __forceinline__ void take(const float *p, float (&x)[N])
             const float4 v = *reinterpret_cast<const float4 *>(p + e);
             x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
         }
+}
+template <int N>
+__device__ __forceinline__ void put(float *p, const float (&x)[N])
+{
+    if constexpr (N == 1) *p = x[0];
+    else if constexpr (N == 2) *reinterpret_cast<float2 *>(p) = make_float2(x[0], x[1]);
+    else *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void la_put4(float *p, const float (&x)[4]) { put<4>(p, x); }
+__device__ __forceinline__ void la_put4(__nv_bfloat16 *p, const float (&x)[4])
+{
+    __nv_bfloat162 y[2] = {__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3])};
+    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<uint2 *>(y);
 }
 // acc[r][c] += sum over k of a[k][r0 + r] b[k][c0 + c]; rows of a and b `sa` and `sb` apart
 template <int R, int N>
@@ -92,7 +105,7 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
     // this thread's tiles: state, output, scores
     const int sr = tid / (VS / L::SC) * L::SR, sc = tid % (VS / L::SC) * L::SC;
     const int orow = tid / (VS / L::OC) * L::OR, oc = tid % (VS / L::OC) * L::OC;
-    const int ar = tid / (CH / L::AC) * L::AR, ac = tid % (CH / L::AC) * L::AC;
+    const int ar = tid % (CH / L::AR) * L::AR, ac = tid / (CH / L::AR) * L::AC;
     float St[L::SR][L::SC];
 #pragma unroll
     for (int r = 0; r < L::SR; ++r)
@@ -102,20 +115,25 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
             St[r][c] = job.s0 != nullptr && d < Dk && e < cols
                            ? job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)] : 0.0f;
         }
-    // a chunk's rows, by way of registers: thread = a column and every (G / width)-th step
+    // a chunk's rows, by way of registers: thread = a column and (of Q, K) groups of four steps, which lie together in the transposes
     constexpr int NQ = CH * DK / G, NV = CH * VS / G, RQ = G / DK, RV = G / VS;
-    const int qi = tid / DK, qd = tid % DK, vi = tid / VS, vc = tid % VS;
+    const int qi = tid / DK * 4, qd = tid % DK, vi = tid / VS, vc = tid % VS;
+    static_assert(NQ % 4 == 0, "groups of four steps");
+    // may four neighbouring outputs be written at once?
+    const bool together = cols % 4 == 0 && ((reinterpret_cast<uintptr_t>(og) | (uintptr_t)(job.o.token * (long long)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
     float rq[NQ], rk[NQ], rv[NV];
     auto fetch = [&](int t0) {
         const long long sign = job.back ? -1 : 1, t = job.back ? n - 1 - t0 : t0;
         const T *pq = qg + (t + sign * qi) * job.q.token + qd, *pk = kg + (t + sign * qi) * job.k.token + qd, *pv = vg + (t + sign * vi) * job.v.token + vc;
-        const long long sq = sign * RQ * job.q.token, sk = sign * RQ * job.k.token, sv = sign * RV * job.v.token;
+        const long long sq = sign * job.q.token, sk = sign * job.k.token, sv = sign * RV * job.v.token;
 #pragma unroll
-        for (int p = 0; p < NQ; ++p, pq += sq, pk += sk) {
-            const bool in = t0 + qi + p * RQ < n && qd < Dk;
-            rq[p] = in ? la_value(pq) : 0.0f;
-            rk[p] = in ? la_value(pk) : 0.0f;
-        }
+        for (int p = 0; p < NQ; p += 4, pq += 4 * RQ * sq, pk += 4 * RQ * sk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = t0 + qi + p * RQ + e < n && qd < Dk;
+                rq[p + e] = in ? la_value(pq + e * sq) : 0.0f;
+                rk[p + e] = in ? la_value(pk + e * sk) : 0.0f;
+            }
 #pragma unroll
         for (int p = 0; p < NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_value(pv) : 0.0f;
     };
@@ -126,11 +144,12 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
         const int rows = min(CH, n - t0);
         __syncthreads();                                     // the chunk before is done with
 #pragma unroll
-        for (int p = 0; p < NQ; ++p) {
-            const int i = qi + p * RQ;
-            qt[qd * L::QS + i] = rq[p];
-            kt[qd * L::QS + i] = rk[p];
-            kw[i * L::KW + qd] = i < rows ? rk[p] * (job.sum_scale * pw[rows - 1 - i]) : 0.0f;
+        for (int p = 0; p < NQ; p += 4) {
+            const int i0 = qi + p * RQ;
+            *reinterpret_cast<float4 *>(qt + qd * L::QS + i0) = make_float4(rq[p], rq[p + 1], rq[p + 2], rq[p + 3]);
+            *reinterpret_cast<float4 *>(kt + qd * L::QS + i0) = make_float4(rk[p], rk[p + 1], rk[p + 2], rk[p + 3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kw[(i0 + e) * L::KW + qd] = i0 + e < rows ? rk[p + e] * (job.sum_scale * pw[rows - 1 - i0 - e]) : 0.0f;
         }
 #pragma unroll
         for (int p = 0; p < NV; ++p) {
@@ -142,22 +161,25 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
             for (int c = 0; c < L::SC; c += 4) *reinterpret_cast<float4 *>(S + (sr + r) * L::VW + sc + c) = make_float4(St[r][c], St[r][c + 1], St[r][c + 2], St[r][c + 3]);
         __syncthreads();
         if (t0 + CH < n) fetch(t0 + CH);
-        {
+        if (ac < rows) {
             float acc[L::AR][L::AC] = {};
             if (ar + L::AR > ac) multiply<L::AR, L::AC>(acc, qt + ar, L::QS, kt + ac, L::QS, DK);          // (above the diagonal there is nothing)
 #pragma unroll
-            for (int r = 0; r < L::AR; ++r)
+            for (int c = 0; c < L::AC; ++c) {
+                float x[L::AR];
 #pragma unroll
-                for (int c = 0; c < L::AC; ++c) {
+                for (int r = 0; r < L::AR; ++r) {
                     const int i = ar + r, j = ac + c;
-                    At[j * L::QS + i] = j <= i && i < rows ? acc[r][c] * (job.sum_scale * pw[i - j]) : 0.0f;
+                    x[r] = j <= i && i < rows ? acc[r][c] * (job.sum_scale * pw[i - j]) : 0.0f;
                 }
+                put<L::AR>(At + (ac + c) * L::QS + ar, x);
+            }
         }
         __syncthreads();
-        {
+        if (orow < rows) {
             float from[L::OR][L::OC] = {}, own[L::OR][L::OC] = {};
             multiply<L::OR, L::OC>(from, qt + orow, L::QS, S + oc, L::VW, DK);
-            multiply<L::OR, L::OC>(own, At + orow, L::QS, v + oc, L::VW, orow + L::OR);
+            multiply<L::OR, L::OC>(own, At + orow, L::QS, v + oc, L::VW, min(orow + L::OR, rows));
 #pragma unroll
             for (int r = 0; r < L::OR; ++r) {
                 const int i = orow + r;
@@ -165,14 +187,20 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
                 const long long t = job.back ? n - 1 - t0 - i : t0 + i;
                 T *const to = og + t * job.o.token + oc;
                 const float f = pw[i + late];
+                float x[L::OC];
 #pragma unroll
-                for (int c = 0; c < L::OC; ++c)
-                    if (oc + c < cols) la_put(to + c, job.out_scale * fmaf(f, from[r][c], own[r][c]));
+                for (int c = 0; c < L::OC; ++c) x[c] = job.out_scale * fmaf(f, from[r][c], own[r][c]);
+                if (together) {
+                    if (oc < cols) la_put4(to, x);
+                } else
+#pragma unroll
+                    for (int c = 0; c < L::OC; ++c)
+                        if (oc + c < cols) la_put(to + c, x[c]);
             }
         }
         const LaStep step(ld, rows - 1 + late);
         float U[L::SR][L::SC] = {};
-        multiply<L::SR, L::SC>(U, kw + sr, L::KW, v + sc, L::VW, CH);
+        multiply<L::SR, L::SC>(U, kw + sr, L::KW, v + sc, L::VW, rows);
 #pragma unroll
         for (int r = 0; r < L::SR; ++r)
 #pragma unroll
