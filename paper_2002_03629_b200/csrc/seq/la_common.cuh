@@ -59,6 +59,35 @@ __device__ __forceinline__ float la_value(const __nv_bfloat16 *p) { return __bfl
 __device__ __forceinline__ void la_put(float *p, float x) { *p = x; }
 __device__ __forceinline__ void la_put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 
+// two fp32 values in a register pair, and operations on both
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float lo, float hi)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float lo(f2 x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float hi(f2 x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 struct LaJobs {
     LaJob job[3];
 };

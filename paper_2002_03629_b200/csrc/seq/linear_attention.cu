@@ -18,67 +18,81 @@ int status(cudaError_t e)
 }
 
 // ------------------------------------------------------------------ any type, size and stride
-// A CTA carries VS columns of the state of one sequence and head through chunks of CH steps, all in fp32 by multiply-adds, sums in a fixed order:
+// A CTA carries VS columns of the state of one sequence and head through chunks of CH steps:
 //     A = (q k^T) * lambda^(i-j), j <= i;     o = A v + lambda^(i+1) q S;     S = lambda^CH S + sum_j lambda^(CH-1-j) k_j v_j^T
-// Bound: the multiply-adds and the shared-memory loads that feed them: tiles of outputs in registers (4 x 4, for the state 4 x 4 to 8 x 8, which
-// stays there), operands in shared memory with the summed index in rows, so that a thread reads its four or eight values in one or two loads.  The next
-// chunk's rows are on their way from memory while this one is computed.  Chunks of 32 steps: twice as long the products of scores would outweigh the
-// others at the widths this path is used for.
+// The products go over warps' matrix instructions of 16 x 8 x 8, every factor as the sum of two TF32 numbers (the upper one rounded; 22 bits in all), the
+// product of the two lower ones left out: off by 3 * 2^-22 of a term at most, sums in fp32 in a fixed order.  (The tiles are too small for the tensor
+// memory path: 32 steps, 32 to 128 values, a 128-row tile would be mostly padding.  By multiply-adds the loads from shared memory were the bound.)
+// Bound: issued instructions, most of them the splitting.  A warp has 16 rows of a product; the state stays in registers; rows are padded so that the
+// lanes of a fragment lie in different banks.  The next chunk's rows are on their way from memory while this one is computed.
 constexpr int CH = 32;
 
 template <int DK, int VS, int G>
 struct AnyTiles {
-    static constexpr int QS = CH + 4;                       // row of q^T, k^T, A^T
-    static constexpr int SR = VS * DK / G / 4 > 8 ? 8 : 4, SC = DK * VS / G / SR;      // the state's tile: rows (Dk) x columns
-    static constexpr int OC = 4, OR = CH * VS / G / OC;     // the output's
-    static constexpr int AC = 4, AR = CH * CH / G / AC;     // the scores', neighbours along i
-    static constexpr int KW = DK + 4, VW = VS + 4;
-    static constexpr int FLOATS = 2 * DK * QS + CH * KW + CH * VW + CH * QS + DK * VW + 2 * CH + 2;
-    static_assert(SC % 4 == 0 && OR >= 1 && AR >= 1, "four columns a load");
+    static constexpr int W = G / 32, CG = W / 2;            // warps: two over a chunk's rows, CG over the columns
+    static constexpr int QW = DK + 8, VW = VS + 8, SW = VS + 4, AW = CH + 4;      // rows of Q and K, V, S, A
+    static constexpr int AN = CH / CG / 8, ON = VS / CG / 8, SN = VS / 8;         // blocks of eight columns of a warp: scores, outputs, state
+    static constexpr int NQ = CH * DK / G / 4, NV = CH * VS / G / 4;              // groups of four values that a thread fetches
+    static constexpr int FLOATS = 2 * CH * QW + CH * VW + DK * SW + CH * AW + 2 * CH + 4;
+    static_assert(AN >= 1 && ON >= 1 && DK == 16 * W, "sixteen rows of the state a warp");
 };
 
-// N neighbouring values of shared memory, on 16 bytes for N >= 4
-template <int N>
-__device__ __forceinline__ void take(const float *p, float (&x)[N])
+// x = h + l, TF32 numbers both, but for 2^-22 x
+__device__ __forceinline__ void split(float x, uint32_t &h, uint32_t &l)
 {
-    if constexpr (N == 1) x[0] = *p;
-    else if constexpr (N == 2) {
-        const float2 v = *reinterpret_cast<const float2 *>(p);
-        x[0] = v.x; x[1] = v.y;
-    } else
+    h = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+    l = __float_as_uint(x - __uint_as_float(h)) & 0xffffe000u;
+}
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+// acc (+)= a b, 16 x 8 N: a(k, x) and b(k, n, y) give this thread's values of the fragments for the eight summed positions from k on
+template <int N, typename FA, typename FB>
+__device__ __forceinline__ void multiply(float (&acc)[N][4], int steps, FA &&a, FB &&b)
+{
+#pragma unroll 1
+    for (int k = 0; k < steps; k += 8) {
+        float x[4];
+        uint32_t xh[4], xl[4];
+        a(k, x);
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(p + e);
-            x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
+        for (int e = 0; e < 4; ++e) split(x[e], xh[e], xl[e]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float y[2];
+            uint32_t yh[2], yl[2];
+            b(k, n, y);
+            split(y[0], yh[0], yl[0]);
+            split(y[1], yh[1], yl[1]);
+            mma_tf32(acc[n], xl, yh);
+            mma_tf32(acc[n], xh, yl);
+            mma_tf32(acc[n], xh, yh);
         }
-}
-template <int N>
-__device__ __forceinline__ void put(float *p, const float (&x)[N])
-{
-    if constexpr (N == 1) *p = x[0];
-    else if constexpr (N == 2) *reinterpret_cast<float2 *>(p) = make_float2(x[0], x[1]);
-    else *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-}
-__device__ __forceinline__ void la_put4(float *p, const float (&x)[4]) { put<4>(p, x); }
-__device__ __forceinline__ void la_put4(__nv_bfloat16 *p, const float (&x)[4])
-{
-    __nv_bfloat162 y[2] = {__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3])};
-    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<uint2 *>(y);
-}
-// acc[r][c] += sum over k of a[k][r0 + r] b[k][c0 + c]; rows of a and b `sa` and `sb` apart
-template <int R, int N>
-__device__ __forceinline__ void multiply(float (&acc)[R][N], const float *a, int sa, const float *b, int sb, int steps)
-{
-#pragma unroll 4
-    for (int k = 0; k < steps; ++k) {
-        float x[R], y[N];
-        take<R>(a + k * sa, x);
-        take<N>(b + k * sb, y);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int c = 0; c < N; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
     }
+}
+// Four neighbouring values, those from `left` on zero; `whole`: may they be read at once?
+__device__ __forceinline__ float4 la_four(const float *p, int left, bool whole)
+{
+    if (whole) return *reinterpret_cast<const float4 *>(p);
+    return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
+}
+__device__ __forceinline__ float4 la_four(const __nv_bfloat16 *p, int left, bool whole)
+{
+    if (whole) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(p);
+        return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u));
+    }
+    return make_float4(left > 0 ? la_value(p) : 0.0f, left > 1 ? la_value(p + 1) : 0.0f, left > 2 ? la_value(p + 2) : 0.0f, left > 3 ? la_value(p + 3) : 0.0f);
+}
+__device__ __forceinline__ void la_put2(float *p, float x, float y) { *reinterpret_cast<float2 *>(p) = make_float2(x, y); }
+__device__ __forceinline__ void la_put2(__nv_bfloat16 *p, float x, float y) { *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(x, y); }
+// do rows of `token` values from p on, `width` of them, consist of whole groups of N values that lie on their own size?
+template <int N, typename T>
+__device__ __forceinline__ bool la_groups(const T *p, long long token, int width)
+{
+    return width % N == 0 && ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(token * (long long)sizeof(T))) & (N * sizeof(T) - 1)) == 0;
 }
 
 template <typename T, int DK, int VS, int G>
@@ -89,8 +103,8 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
     const LaJob &job = jobs.job[blockIdx.z];
     const int Dk = job.Dk, c0 = blockIdx.y * VS, tid = threadIdx.x;
     if (c0 >= job.Dv) return;
-    float *const qt = sm, *const kt = qt + DK * L::QS, *const kw = kt + DK * L::QS, *const v = kw + CH * L::KW, *const At = v + CH * L::VW, *const S = At + CH * L::QS,
-          *const pw = S + DK * L::VW;                        // pw[n] = lambda^n, n <= CH
+    float *const q = sm, *const k = q + CH * L::QW, *const v = k + CH * L::QW, *const St = v + CH * L::VW, *const A = St + DK * L::SW,
+          *const pw = A + CH * L::AW, *const wk = pw + CH + 4;           // pw[n] = lambda^n, n <= CH; weights of K's rows
     const int cols = min(VS, job.Dv - c0), seq = blockIdx.x / seqs.H, h = blockIdx.x % seqs.H;
     long long start;
     const int n = la_sequence(seqs, seq, start);
@@ -102,40 +116,37 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
     T *const og = (T *)job.o.data + b * job.o.batch + start * job.o.token + h * job.o.head + c0;
     const size_t sbase = (size_t)blockIdx.x * Dk * job.Dv;
     for (int p = tid; p <= CH; p += G) pw[p] = la_power(ld, p);
-    // this thread's tiles: state, output, scores
-    const int sr = tid / (VS / L::SC) * L::SR, sc = tid % (VS / L::SC) * L::SC;
-    const int orow = tid / (VS / L::OC) * L::OR, oc = tid % (VS / L::OC) * L::OC;
-    const int ar = tid % (CH / L::AR) * L::AR, ac = tid / (CH / L::AR) * L::AC;
-    float St[L::SR][L::SC];
+    // this thread's place in a fragment; the warp's rows of a chunk, and its columns of the scores and outputs; its rows of the state
+    const int warp = tid / 32, g = tid / 4 % 8, t = tid % 4;
+    const int row0 = warp % 2 * 16, ac = warp / 2 * 8 * L::AN, oc = warp / 2 * 8 * L::ON, i0 = row0 + g, d0 = 16 * warp + g;
+    float S[L::SN][4];
 #pragma unroll
-    for (int r = 0; r < L::SR; ++r)
+    for (int b = 0; b < L::SN; ++b)
 #pragma unroll
-        for (int c = 0; c < L::SC; ++c) {
-            const int d = sr + r, e = sc + c;
-            St[r][c] = job.s0 != nullptr && d < Dk && e < cols
-                           ? job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)] : 0.0f;
+        for (int x = 0; x < 4; ++x) {
+            const int d = d0 + x / 2 * 8, e = 8 * b + 2 * t + x % 2;
+            S[b][x] = job.s0 != nullptr && d < Dk && e < cols
+                          ? job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)] : 0.0f;
         }
-    // a chunk's rows, by way of registers: thread = a column and (of Q, K) groups of four steps, which lie together in the transposes
-    constexpr int NQ = CH * DK / G, NV = CH * VS / G, RQ = G / DK, RV = G / VS;
-    const int qi = tid / DK * 4, qd = tid % DK, vi = tid / VS, vc = tid % VS;
-    static_assert(NQ % 4 == 0, "groups of four steps");
-    // may four neighbouring outputs be written at once?
-    const bool together = cols % 4 == 0 && ((reinterpret_cast<uintptr_t>(og) | (uintptr_t)(job.o.token * (long long)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
-    float rq[NQ], rk[NQ], rv[NV];
+    // a chunk's rows, by way of registers: thread = four columns and every eighth (V: RV-th) step
+    constexpr int RQ = 4 * G / DK, RV = 4 * G / VS;
+    const int qi = tid / (DK / 4), qd = tid % (DK / 4) * 4, vi = tid / (VS / 4), vc = tid % (VS / 4) * 4;
+    const bool q4 = la_groups<4>(qg, job.q.token, Dk) && la_groups<4>(kg, job.k.token, Dk), v4 = la_groups<4>(vg, job.v.token, cols);
+    const bool o2 = la_groups<2>(og, job.o.token, cols);
+    float4 rq[L::NQ], rk[L::NQ], rv[L::NV];
     auto fetch = [&](int t0) {
-        const long long sign = job.back ? -1 : 1, t = job.back ? n - 1 - t0 : t0;
-        const T *pq = qg + (t + sign * qi) * job.q.token + qd, *pk = kg + (t + sign * qi) * job.k.token + qd, *pv = vg + (t + sign * vi) * job.v.token + vc;
-        const long long sq = sign * job.q.token, sk = sign * job.k.token, sv = sign * RV * job.v.token;
+        const long long sign = job.back ? -1 : 1, at = job.back ? n - 1 - t0 : t0;
+        const T *pq = qg + (at + sign * qi) * job.q.token + qd, *pk = kg + (at + sign * qi) * job.k.token + qd, *pv = vg + (at + sign * vi) * job.v.token + vc;
+        const long long sq = sign * RQ * job.q.token, sk = sign * RQ * job.k.token, sv = sign * RV * job.v.token;
+        const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int p = 0; p < NQ; p += 4, pq += 4 * RQ * sq, pk += 4 * RQ * sk)
+        for (int p = 0; p < L::NQ; ++p, pq += sq, pk += sk) {
+            const bool in = t0 + qi + p * RQ < n && qd < Dk;
+            rq[p] = in ? la_four(pq, Dk - qd, q4) : zero;
+            rk[p] = in ? la_four(pk, Dk - qd, q4) : zero;
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool in = t0 + qi + p * RQ + e < n && qd < Dk;
-                rq[p + e] = in ? la_value(pq + e * sq) : 0.0f;
-                rk[p + e] = in ? la_value(pk + e * sk) : 0.0f;
-            }
-#pragma unroll
-        for (int p = 0; p < NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_value(pv) : 0.0f;
+        for (int p = 0; p < L::NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_four(pv, cols - vc, v4) : zero;
     };
     if (n > 0) fetch(0);
     int late = job.back ? 0 : 1;
@@ -144,75 +155,105 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
         const int rows = min(CH, n - t0);
         __syncthreads();                                     // the chunk before is done with
 #pragma unroll
-        for (int p = 0; p < NQ; p += 4) {
-            const int i0 = qi + p * RQ;
-            *reinterpret_cast<float4 *>(qt + qd * L::QS + i0) = make_float4(rq[p], rq[p + 1], rq[p + 2], rq[p + 3]);
-            *reinterpret_cast<float4 *>(kt + qd * L::QS + i0) = make_float4(rk[p], rk[p + 1], rk[p + 2], rk[p + 3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) kw[(i0 + e) * L::KW + qd] = i0 + e < rows ? rk[p + e] * (job.sum_scale * pw[rows - 1 - i0 - e]) : 0.0f;
+        for (int p = 0; p < L::NQ; ++p) {
+            *reinterpret_cast<float4 *>(q + (qi + p * RQ) * L::QW + qd) = rq[p];
+            *reinterpret_cast<float4 *>(k + (qi + p * RQ) * L::QW + qd) = rk[p];
         }
 #pragma unroll
-        for (int p = 0; p < NV; ++p) {
-            v[(vi + p * RV) * L::VW + vc] = rv[p];
+        for (int p = 0; p < L::NV; ++p) *reinterpret_cast<float4 *>(v + (vi + p * RV) * L::VW + vc) = rv[p];
+#pragma unroll
+        for (int b = 0; b < L::SN; ++b) {
+            *reinterpret_cast<float2 *>(St + d0 * L::SW + 8 * b + 2 * t) = make_float2(S[b][0], S[b][1]);
+            *reinterpret_cast<float2 *>(St + (d0 + 8) * L::SW + 8 * b + 2 * t) = make_float2(S[b][2], S[b][3]);
         }
-#pragma unroll
-        for (int r = 0; r < L::SR; ++r)
-#pragma unroll
-            for (int c = 0; c < L::SC; c += 4) *reinterpret_cast<float4 *>(S + (sr + r) * L::VW + sc + c) = make_float4(St[r][c], St[r][c + 1], St[r][c + 2], St[r][c + 3]);
+        if (tid < CH) wk[tid] = tid < rows ? job.sum_scale * pw[rows - 1 - tid] : 0.0f;
         __syncthreads();
         if (t0 + CH < n) fetch(t0 + CH);
-        if (ac < rows) {
-            float acc[L::AR][L::AC] = {};
-            if (ar + L::AR > ac) multiply<L::AR, L::AC>(acc, qt + ar, L::QS, kt + ac, L::QS, DK);          // (above the diagonal there is nothing)
+        auto q_rows = [&](int at, float (&x)[4]) {           // (neighbours of the summed index in one load)
+            const float2 a = *reinterpret_cast<const float2 *>(q + i0 * L::QW + at + 2 * t), b = *reinterpret_cast<const float2 *>(q + (i0 + 8) * L::QW + at + 2 * t);
+            x[0] = a.x; x[1] = b.x; x[2] = a.y; x[3] = b.y;
+        };
+        if (row0 < rows) {
+            float acc[L::AN][4] = {};
+            if (ac < row0 + 16)                              // (else above the diagonal)
+                multiply<L::AN>(acc, DK, q_rows, [&](int at, int b, float (&y)[2]) {
+                    const float2 x = *reinterpret_cast<const float2 *>(k + (ac + 8 * b + g) * L::QW + at + 2 * t);
+                    y[0] = x.x; y[1] = x.y;
+                });
 #pragma unroll
-            for (int c = 0; c < L::AC; ++c) {
-                float x[L::AR];
+            for (int b = 0; b < L::AN; ++b)
 #pragma unroll
-                for (int r = 0; r < L::AR; ++r) {
-                    const int i = ar + r, j = ac + c;
-                    x[r] = j <= i && i < rows ? acc[r][c] * (job.sum_scale * pw[i - j]) : 0.0f;
+                for (int x = 0; x < 2; ++x) {
+                    const int i = i0 + 8 * x, j = ac + 8 * b + 2 * t;
+                    *reinterpret_cast<float2 *>(A + i * L::AW + j) = make_float2(j <= i && i < rows ? acc[b][2 * x] * (job.sum_scale * pw[i - j]) : 0.0f,
+                                                                                 j < i && i < rows ? acc[b][2 * x + 1] * (job.sum_scale * pw[i - j - 1]) : 0.0f);
                 }
-                put<L::AR>(At + (ac + c) * L::QS + ar, x);
-            }
         }
         __syncthreads();
-        if (orow < rows) {
-            float from[L::OR][L::OC] = {}, own[L::OR][L::OC] = {};
-            multiply<L::OR, L::OC>(from, qt + orow, L::QS, S + oc, L::VW, DK);
-            multiply<L::OR, L::OC>(own, At + orow, L::QS, v + oc, L::VW, min(orow + L::OR, rows));
+        if (row0 < rows) {
+            float o[L::ON][4] = {};
+            multiply<L::ON>(o, DK, q_rows, [&](int at, int b, float (&y)[2]) {
+                const float *const x = St + (at + 2 * t) * L::SW + oc + 8 * b + g;
+                y[0] = x[0]; y[1] = x[L::SW];
+            });
+            const float f[2] = {pw[min(i0 + late, CH)], pw[min(i0 + 8 + late, CH)]};
 #pragma unroll
-            for (int r = 0; r < L::OR; ++r) {
-                const int i = orow + r;
+            for (int b = 0; b < L::ON; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[b][x] *= f[x / 2];
+            multiply<L::ON>(o, min(row0 + 16, rows),
+                            [&](int at, float (&x)[4]) {
+                                const float *const a = A + i0 * L::AW + at + t;
+                                x[0] = a[0]; x[1] = a[8 * L::AW]; x[2] = a[4]; x[3] = a[8 * L::AW + 4];
+                            },
+                            [&](int at, int b, float (&y)[2]) {
+                                const float *const x = v + (at + t) * L::VW + oc + 8 * b + g;
+                                y[0] = x[0]; y[1] = x[4 * L::VW];
+                            });
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int i = i0 + 8 * x;
                 if (i >= rows) continue;
-                const long long t = job.back ? n - 1 - t0 - i : t0 + i;
-                T *const to = og + t * job.o.token + oc;
-                const float f = pw[i + late];
-                float x[L::OC];
+                T *const to = og + (job.back ? n - 1 - t0 - i : t0 + i) * job.o.token + oc + 2 * t;
 #pragma unroll
-                for (int c = 0; c < L::OC; ++c) x[c] = job.out_scale * fmaf(f, from[r][c], own[r][c]);
-                if (together) {
-                    if (oc < cols) la_put4(to, x);
-                } else
-#pragma unroll
-                    for (int c = 0; c < L::OC; ++c)
-                        if (oc + c < cols) la_put(to + c, x[c]);
+                for (int b = 0; b < L::ON; ++b) {
+                    const float y = job.out_scale * o[b][2 * x], z = job.out_scale * o[b][2 * x + 1];
+                    const int left = cols - oc - 2 * t - 8 * b;
+                    if (o2) {
+                        if (left > 0) la_put2(to + 8 * b, y, z);
+                    } else {
+                        if (left > 0) la_put(to + 8 * b, y);
+                        if (left > 1) la_put(to + 8 * b + 1, z);
+                    }
+                }
             }
         }
         const LaStep step(ld, rows - 1 + late);
-        float U[L::SR][L::SC] = {};
-        multiply<L::SR, L::SC>(U, kw + sr, L::KW, v + sc, L::VW, rows);
+        float U[L::SN][4] = {};
+        multiply<L::SN>(U, rows,
+                        [&](int at, float (&x)[4]) {
+                            const float *const a = k + (at + t) * L::QW + d0;
+                            const float w = wk[at + t], u = wk[at + t + 4];
+                            x[0] = w * a[0]; x[1] = w * a[8]; x[2] = u * a[4 * L::QW]; x[3] = u * a[4 * L::QW + 8];
+                        },
+                        [&](int at, int b, float (&y)[2]) {
+                            const float *const x = v + (at + t) * L::VW + 8 * b + g;
+                            y[0] = x[0]; y[1] = x[4 * L::VW];
+                        });
 #pragma unroll
-        for (int r = 0; r < L::SR; ++r)
+        for (int b = 0; b < L::SN; ++b)
 #pragma unroll
-            for (int c = 0; c < L::SC; ++c) St[r][c] = step(St[r][c], U[r][c]);
+            for (int x = 0; x < 4; ++x) S[b][x] = step(S[b][x], U[b][x]);
     }
     if (job.s1 == nullptr) return;
     const float last = job.back && n > 0 ? la_power(ld, 1) : 1.0f;
 #pragma unroll
-    for (int r = 0; r < L::SR; ++r)
+    for (int b = 0; b < L::SN; ++b)
 #pragma unroll
-        for (int c = 0; c < L::SC; ++c)
-            if (sr + r < Dk && sc + c < cols) job.s1[sbase + (size_t)(sr + r) * job.Dv + c0 + sc + c] = last * St[r][c];
+        for (int x = 0; x < 4; ++x) {
+            const int d = d0 + x / 2 * 8, e = 8 * b + 2 * t + x % 2;
+            if (d < Dk && e < cols) job.s1[sbase + (size_t)d * job.Dv + c0 + e] = last * S[b][x];
+        }
 }
 
 // ------------------------------------------------------------------ single steps
