@@ -48,10 +48,13 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], 
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// acc (+)= a b, 16 x 8 N: a(k, x) and b(k, n, y) give this thread's values of the fragments for the eight summed positions from k on
+// acc += a b, 16 x 8 N: a(k, x) and b(k, n, y) give this thread's values of the fragments for the eight summed positions from k on.  (The
+// instruction's sums are cut towards zero: the lower numbers' products have a sum of their own, so that the upper ones' is cut once in eight terms.
+// All in one sum a prompt of 100 steps, 8 heads of 64, came out 7e-7 off.)
 template <int N, typename FA, typename FB>
 __device__ __forceinline__ void multiply(float (&acc)[N][4], int steps, FA &&a, FB &&b)
 {
+    float low[N][4] = {};
 #pragma unroll 1
     for (int k = 0; k < steps; k += 8) {
         float x[4];
@@ -66,11 +69,15 @@ __device__ __forceinline__ void multiply(float (&acc)[N][4], int steps, FA &&a, 
             b(k, n, y);
             split(y[0], yh[0], yl[0]);
             split(y[1], yh[1], yl[1]);
-            mma_tf32(acc[n], xl, yh);
-            mma_tf32(acc[n], xh, yl);
+            mma_tf32(low[n], xl, yh);
             mma_tf32(acc[n], xh, yh);
+            mma_tf32(low[n], xh, yl);
         }
     }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][e] += low[n][e];
 }
 // Four neighbouring values, those from `left` on zero; `whole`: may they be read at once?
 __device__ __forceinline__ float4 la_four(const float *p, int left, bool whole)
@@ -96,7 +103,7 @@ __device__ __forceinline__ bool la_groups(const T *p, long long token, int width
 }
 
 template <typename T, int DK, int VS, int G>
-__global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
+__global__ void __launch_bounds__(G, DK == 32 ? 6 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
 {
     using L = AnyTiles<DK, VS, G>;
     extern __shared__ __align__(16) float sm[];
@@ -229,21 +236,24 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
             }
         }
         const LaStep step(ld, rows - 1 + late);
-        float U[L::SN][4] = {};
-        multiply<L::SN>(U, rows,
+#pragma unroll
+        for (int b0 = 0; b0 < L::SN; b0 += 4) {
+            float U[4][4] = {};
+            multiply<4>(U, rows,
                         [&](int at, float (&x)[4]) {
                             const float *const a = k + (at + t) * L::QW + d0;
                             const float w = wk[at + t], u = wk[at + t + 4];
                             x[0] = w * a[0]; x[1] = w * a[8]; x[2] = u * a[4 * L::QW]; x[3] = u * a[4 * L::QW + 8];
                         },
                         [&](int at, int b, float (&y)[2]) {
-                            const float *const x = v + (at + t) * L::VW + 8 * b + g;
+                            const float *const x = v + (at + t) * L::VW + 8 * (b0 + b) + g;
                             y[0] = x[0]; y[1] = x[4 * L::VW];
                         });
 #pragma unroll
-        for (int b = 0; b < L::SN; ++b)
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) S[b][x] = step(S[b][x], U[b][x]);
+                for (int x = 0; x < 4; ++x) S[b0 + b][x] = step(S[b0 + b][x], U[b][x]);
+        }
     }
     if (job.s1 == nullptr) return;
     const float last = job.back && n > 0 ? la_power(ld, 1) : 1.0f;
