@@ -23,8 +23,11 @@ int status(cudaError_t e)
 // The products go over warps' matrix instructions of 16 x 8 x 8, every factor as the sum of two TF32 numbers (the upper one rounded; 22 bits in all), the
 // product of the two lower ones left out: off by 3 * 2^-22 of a term at most, sums in fp32 in a fixed order.  (The tiles are too small for the tensor
 // memory path: 32 steps, 32 to 128 values, a 128-row tile would be mostly padding.  By multiply-adds the loads from shared memory were the bound.)
-// Bound: issued instructions, most of them the splitting.  A warp has 16 rows of a product; the state stays in registers; rows are padded so that the
-// lanes of a fragment lie in different banks.  The next chunk's rows are on their way from memory while this one is computed.
+// Bound: issued instructions (half of all slots; most are the splitting) and waits for them, tensor pipe at 37 %, DRAM at 24 %.  A warp has 16 rows of a
+// product; the state stays in registers; rows are padded so that the lanes of a fragment lie in different banks.  Rows fetched a chunk ahead into
+// registers cost two CTAs an SM: 168 us in place of 159.
+// Measured: gradients of 592 x 100 steps, 4 heads of 32, fp32: 159 us (multiply-adds 221; 454 MB at least, 2.9 TB/s); one prompt of 100 steps, 8 heads
+// of 64: 13.5 us, the latency of four chunks after one another.
 constexpr int CH = 32;
 
 template <int DK, int VS, int G>
@@ -55,7 +58,7 @@ template <int N, typename FA, typename FB>
 __device__ __forceinline__ void multiply(float (&acc)[N][4], int steps, FA &&a, FB &&b)
 {
     float low[N][4] = {};
-#pragma unroll 1
+#pragma unroll 2
     for (int k = 0; k < steps; k += 8) {
         float x[4];
         uint32_t xh[4], xl[4];
@@ -103,7 +106,7 @@ __device__ __forceinline__ bool la_groups(const T *p, long long token, int width
 }
 
 template <typename T, int DK, int VS, int G>
-__global__ void __launch_bounds__(G, DK == 32 ? 6 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
+__global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
 {
     using L = AnyTiles<DK, VS, G>;
     extern __shared__ __align__(16) float sm[];
@@ -155,11 +158,11 @@ __global__ void __launch_bounds__(G, DK == 32 ? 6 : DK == 64 ? 3 : 2) la_any_ker
 #pragma unroll
         for (int p = 0; p < L::NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_four(pv, cols - vc, v4) : zero;
     };
-    if (n > 0) fetch(0);
     int late = job.back ? 0 : 1;
 #pragma unroll 1
     for (int t0 = 0; t0 < n; t0 += CH, late = 1) {
         const int rows = min(CH, n - t0);
+        fetch(t0);
         __syncthreads();                                     // the chunk before is done with
 #pragma unroll
         for (int p = 0; p < L::NQ; ++p) {
@@ -175,7 +178,6 @@ __global__ void __launch_bounds__(G, DK == 32 ? 6 : DK == 64 ? 3 : 2) la_any_ker
         }
         if (tid < CH) wk[tid] = tid < rows ? job.sum_scale * pw[rows - 1 - tid] : 0.0f;
         __syncthreads();
-        if (t0 + CH < n) fetch(t0 + CH);
         auto q_rows = [&](int at, float (&x)[4]) {           // (neighbours of the summed index in one load)
             const float2 a = *reinterpret_cast<const float2 *>(q + i0 * L::QW + at + 2 * t), b = *reinterpret_cast<const float2 *>(q + (i0 + 8) * L::QW + at + 2 * t);
             x[0] = a.x; x[1] = b.x; x[2] = a.y; x[3] = b.y;
@@ -363,7 +365,8 @@ template <typename T>
 cudaError_t run_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dk, int dv, cudaStream_t stream)
 {
     if (dk <= 32) return launch_any<T, 32, 32, 64>(jobs, seqs, count, dv, stream);
-    // (few of them: halves of the state's columns, one prompt of 100 steps, 8 heads of 64: 29 -> 21 us)
+    // (few sequences and heads: two CTAs a head, a half of the state's columns each, while all of them have an SM of their own; one prompt of 100 steps,
+    // 8 heads of 64: 13.5 us for 19)
     const bool few = (long long)seqs.n * seqs.H * count * 2 <= 148;
     if (dk <= 64) return dv <= 32 || few ? launch_any<T, 64, 32, 128>(jobs, seqs, count, dv, stream) : launch_any<T, 64, 64, 128>(jobs, seqs, count, dv, stream);
     return launch_any<T, 128, 64, 256>(jobs, seqs, count, dv, stream);
