@@ -19,15 +19,18 @@
  * written may not overlap one that is read.
  *
  * Types: LA_F32 or LA_BF16 for q, k, v, o and their gradients; sums and states are fp32.  Where bf16 rows lie on 16 bytes (base and strides)
- * and Dk, Dv are multiples of 16, and in la_forward and la_backward only, the products run on the tensor cores; the intermediate
- * scores and the state that a chunk starts from are then rounded to bf16 before their product.
+ * and Dk, Dv are multiples of 16, and in la_forward and la_backward only, the products take bf16 factors: the intermediate
+ * scores and the state that a chunk starts from are rounded to bf16 before their product, the sums that a state is made of are not (its factors go in
+ * two or three bf16 pieces: off by 3e-6 in the first case, which is taken where no state is asked for or the chunk is too far back to be seen in
+ * it).  Everywhere else the products are of fp32 values in two pieces of 22 bits together.
  * Values that are not finite: outputs of the chunk of up to 128 steps that holds one, and everything that depends on it, are not specified; no
  * other sequence and no other head is touched.
  *
  * Asynchronous on `stream`, allocates nothing; the same call gives the same bits.  `workspace`: device memory of la_workspace() bytes on
  * 16 bytes, used by this call until its work on the stream is done (calls on different streams, and graphs that may run
  * at the same time, need one each).  Limits: 1 <= Dk, Dv <= LA_MAX_D, H >= 1, B, N >= 0, sequences * H <= 2^24, B * T <= 2^40, T <= 2^31 - 1.
- * Returns LA_OK, LA_ERR_INVALID (nothing is launched) or LA_ERR_CUDA (la_last_error() names the error).
+ * Waits inside the kernels, for their own copies and products, end after two seconds; outputs that were not written by then are undefined,
+ * the states NaN.  Returns LA_OK, LA_ERR_INVALID (nothing is launched) or LA_ERR_CUDA (la_last_error() names the error).
  */
 #ifndef LINEAR_ATTENTION_H
 #define LINEAR_ATTENTION_H
@@ -41,7 +44,6 @@ extern "C" {
 #define LA_OK 0
 #define LA_ERR_INVALID (-1)
 #define LA_ERR_CUDA (-2)
-#define LA_ERR_TIMEOUT (-3)
 #define LA_MAX_D 128
 #define LA_F32 0
 #define LA_BF16 1

@@ -5,6 +5,7 @@
 // in the chunk, weights w_j = lambda^(rows-1-j) and the state S before it:
 //     scores = Q K^T;   P = scores * lambda^(i-j), j <= i;   U = (w K)^T V;   O = lambda^(i+1) (Q S) + P V;   S = lambda^rows S + U
 // Backwards in time the tiles lie in memory order all the same and the position of row r is rows-1-r.
+// Packed sequences: a kernel of one CTA sorts them by length, and the CTAs take the next unit as they come free.
 // Roles:
 //   P, O  four warps: scores from tensor memory, masked and decayed, as bf16 back over them (the left operand of P V); then the chunk before's
 //         outputs to memory.  Under strong decay Q S is scaled by lambda^(i+1) in tensor memory before P V is added.
@@ -13,6 +14,10 @@
 //         tensor memory, the third back to where K was.  The state, fp32, in registers, a row of Dv / 2 values a thread; rounded to bf16 into shared
 //         memory for Q S.
 //   a warp that finds units and loads tiles (TMA, a ring of stages that runs on across chunks and units), one that issues the MMAs
+// Bound: the chain of the roles from one chunk to the next, 4.2 us a chunk and SM at widths of 128 (tensor pipe active for 28 % of the time, issue slots
+// for 35 %, DRAM for 30 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
+// Measured, bf16, 16 heads of 128: one prompt of 65536 steps 340 us (own states 83, their chain 10, outputs 245; 1.07 GB, 3.2 TB/s); gradients of 8 x 2048
+// steps 214 us; 20 packed prompts of 1 to 2500 steps 102 us (196 with the units dealt out beforehand).
 // Tensor memory is full: scores and P over them, U, O and K's pieces take 128 columns each.
 // The roles' loops are kept short and free of what can be done once: unrolled further, or with the search for units in each of them, their code
 // fell out of the instruction cache.  setmaxnreg for one role with a whole row of the state a thread was slower (20 warps, spills in others).

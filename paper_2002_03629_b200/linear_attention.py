@@ -9,7 +9,7 @@ import torch
 
 from .binding import JsError, JS_ERR_ARG, load_library, _elsewhere, _stream_ptr, _there
 
-LA_OK, LA_ERR_INVALID, LA_ERR_CUDA, LA_ERR_TIMEOUT = 0, -1, -2, -3
+LA_OK, LA_ERR_INVALID, LA_ERR_CUDA = 0, -1, -2
 LA_MAX_D = 128
 LA_F32, LA_BF16 = 0, 1
 _TYPES = {torch.float32: LA_F32, torch.bfloat16: LA_BF16}
