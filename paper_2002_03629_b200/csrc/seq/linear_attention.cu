@@ -356,8 +356,10 @@ cudaError_t launch_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dv
 {
     auto kernel = la_any_kernel<T, DK, VS, G>;
     constexpr size_t smem = AnyTiles<DK, VS, G>::FLOATS * sizeof(float);
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    if constexpr (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     kernel<<<dim3((unsigned)(seqs.n * seqs.H), (dv + VS - 1) / VS, count), G, smem, stream>>>(jobs, seqs);
     return cudaGetLastError();
 }

@@ -111,11 +111,11 @@ def _shape(q, v, log_decay, scale, cu_seqlens, dims=4):
     return s, n, index
 
 
-def _workspace(s, backward, device):
+def _workspace(s, backward, like):
     n = _lib().la_workspace(s, backward)
     if n == 0:
         _bad(f"sizes outside the documented limits (1 <= Dk, Dv <= {LA_MAX_D})")
-    return torch.empty((n,), dtype=torch.uint8, device=device), n
+    return like.new_empty((n + 3) // 4), n
 
 
 def linear_attention(q, k, v, log_decay, scale: float = 1.0, state=None, cu_seqlens=None, need_state: bool = True, out=None, stream=None):
@@ -127,21 +127,21 @@ def linear_attention(q, k, v, log_decay, scale: float = 1.0, state=None, cu_seql
     s, n, index = _shape(q, v, log_decay, scale, cu_seqlens)
     if _elsewhere(index, stream):
         with _there(index, stream):
-            return _forward(s, n, index, q, k, v, state, need_state, out)
-    return _forward(s, n, index, q, k, v, state, need_state, out)
+            return _forward(s, n, index, q, k, v, log_decay, state, need_state, out)
+    return _forward(s, n, index, q, k, v, log_decay, state, need_state, out)
 
 
-def _forward(s, n, index, q, k, v, state, need_state, out):
-    (B, T, H, Dk), Dv, dtype, device = q.shape, v.shape[-1], q.dtype, q.device
+def _forward(s, n, index, q, k, v, log_decay, state, need_state, out):
+    (B, T, H, Dk), Dv, dtype = q.shape, v.shape[-1], q.dtype
     if out is None:
-        out = torch.empty((B, T, H, Dv), dtype=dtype, device=device)
+        out = q.new_empty((B, T, H, Dv))
         to = _pack_tensor(out.data_ptr(), T * H * Dv, H * Dv, Dv)
     else:
         to = _tensor(out, dtype, index, (B, T, H, Dv), "out", True)
     args = [_tensor(t, dtype, index, (B, T, H, d), w) for t, d, w in ((q, Dk, "q"), (k, Dk, "k"), (v, Dv, "v"))]
     s0 = _state(state, (n, H, Dk, Dv), index, "state")
-    S = torch.empty((n, H, Dk, Dv), dtype=torch.float32, device=device) if need_state else None
-    ws, size = _workspace(s, 0, device)
+    S = log_decay.new_empty((n, H, Dk, Dv)) if need_state else None
+    ws, size = _workspace(s, 0, log_decay)
     _check(_lib().la_forward(s, *args, s0, to, S.data_ptr() if need_state else None, ws.data_ptr(), size, _stream_ptr(None)), "linear_attention")
     return out, S
 
@@ -152,19 +152,19 @@ def linear_attention_backward(q, k, v, log_decay, do, scale: float = 1.0, state=
     s, n, index = _shape(q, v, log_decay, scale, cu_seqlens)
     if _elsewhere(index, stream):
         with _there(index, stream):
-            return _backward(s, n, index, q, k, v, do, state, dstate, cu_seqlens is not None)
-    return _backward(s, n, index, q, k, v, do, state, dstate, cu_seqlens is not None)
+            return _backward(s, n, index, q, k, v, log_decay, do, state, dstate, cu_seqlens is not None)
+    return _backward(s, n, index, q, k, v, log_decay, do, state, dstate, cu_seqlens is not None)
 
 
-def _backward(s, n, index, q, k, v, do, state, dstate, packed):
-    (B, T, H, Dk), Dv, dtype, device = q.shape, v.shape[-1], q.dtype, q.device
+def _backward(s, n, index, q, k, v, log_decay, do, state, dstate, packed):
+    (B, T, H, Dk), Dv, dtype = q.shape, v.shape[-1], q.dtype
     ins = [_tensor(t, dtype, index, (B, T, H, d), w) for t, d, w in ((q, Dk, "q"), (k, Dk, "k"), (v, Dv, "v"), (do, Dv, "do"))]
     s0, ds = _state(state, (n, H, Dk, Dv), index, "state"), _state(dstate, (n, H, Dk, Dv), index, "dstate")
-    make = torch.zeros if packed else torch.empty
-    grads = [make((B, T, H, d), dtype=dtype, device=device) for d in (Dk, Dk, Dv)]
+    make = q.new_zeros if packed else q.new_empty
+    grads = [make((B, T, H, d)) for d in (Dk, Dk, Dv)]
     outs = [_pack_tensor(t.data_ptr(), T * H * d, H * d, d) for t, d in zip(grads, (Dk, Dk, Dv))]
-    dS0 = torch.empty((n, H, Dk, Dv), dtype=torch.float32, device=device)
-    ws, size = _workspace(s, 1, device)
+    dS0 = log_decay.new_empty((n, H, Dk, Dv))
+    ws, size = _workspace(s, 1, log_decay)
     _check(_lib().la_backward(s, *ins[:3], s0, ins[3], ds, *outs, dS0.data_ptr(), ws.data_ptr(), size, _stream_ptr(None)), "linear_attention_backward")
     return (*grads, dS0)
 
@@ -183,7 +183,7 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0, out=Non
 def _step(s, index, q, k, v, state, out):
     (B, H, Dk), Dv, dtype = q.shape, v.shape[-1], q.dtype
     if out is None:
-        out = torch.empty((B, H, Dv), dtype=dtype, device=q.device)
+        out = q.new_empty((B, H, Dv))
         to = _pack_tensor(out.data_ptr(), H * Dv, 0, Dv)
     else:
         to = _tensor(out, dtype, index, (B, H, Dv), "out", True)

@@ -62,11 +62,10 @@ def policy_loss(logits, actions, old_logp, advantages, weights=None, ref_logp=No
         raise JsError(JS_ERR_ARG, "actions, old_logp and advantages are needed")
     rows = [_row(t, N, f32 if i else torch.int64, index, w) for i, (t, w) in
             enumerate(((actions, "actions"), (old_logp, "old_logp"), (advantages, "advantages"), (weights, "weights"), (ref_logp, "ref_logp")))]
-    loss = torch.empty((N,), dtype=f32, device=logits.device)
-    logp = torch.empty_like(loss)
+    loss, logp = torch.empty_like(old_logp), torch.empty_like(old_logp)
     d, dstride = None, 0
     if dlogits is None and need_grad:
-        dlogits = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+        dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
         d, dstride = dlogits.data_ptr(), V
     elif dlogits is not None:
         d, dstride = _matrix(dlogits, "dlogits")
