@@ -122,7 +122,7 @@ struct Out {                                 // where a stage's output goes: job
 };
 
 struct Shared {
-    uint64_t full[4], empty[4], staged[4], told[RING], heard[RING];
+    uint64_t full[4], q_full[4], empty[4], staged[4], told[RING], heard[RING];      // full: K and V
     uint64_t sc_full, p_ready, k_ready, low_ready, s_ready, qs_done, u_full, u_free, o_scaled, o_full, o_free;
     Work work[RING];
     Out out[4];
@@ -190,10 +190,12 @@ __device__ __forceinline__ void stsm4_t(uint32_t at, const uint32_t (&r)[4])
 {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// Eight columns of sixteen lanes over a warp: lane i holds column i % 4 of lanes i / 4 (r[0]) and i / 4 + 8 (r[1]), and the same of the next four columns
-__device__ __forceinline__ void tmem_st_16x8(uint32_t taddr, const uint32_t (&r)[4])
+// Sixteen columns of sixteen lanes over a warp: lane i holds column i % 4 of lanes i / 4 (r[0]) and i / 4 + 8 (r[1]), and the same of the next columns,
+// four at a time
+__device__ __forceinline__ void tmem_st_16x16(uint32_t taddr, const uint32_t (&r)[8])
 {
-    asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap *map, uint32_t src, int c0, int c1, int c2, int c3)
 {
@@ -227,7 +229,7 @@ __device__ __forceinline__ void p_pack(uint32_t (&s)[32], uint32_t (&w)[16], con
         w[e / 2] = narrow(r.x);
         w[e / 2 + 1] = narrow(r.y);
     }
-    if (keep != 0xffffffffu)
+    if (keep != 0xffffffffu)                                 // (the row's own block, and the last ones of a ragged chunk)
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] &= (keep >> (2 * e) & 1u ? 0xffffu : 0u) | (keep >> (2 * e + 1) & 1u ? 0xffff0000u : 0u);
 }
@@ -265,19 +267,17 @@ __device__ __forceinline__ void k_pieces(uint32_t from, const uint32_t (&shift)[
 #pragma unroll
             for (int g = 0; g < 2; ++g) ldsm4_t(from + (uint32_t)(q * 2048) + shift[g], k[q][g]);
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int g = 0; g < 2; ++g) {
+            uint32_t h[8], m[8];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                uint32_t h[4], m[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 kk = as_bf2(k[q][g][e]), a = as_bf2(w1[2 * q + (e >> 1)]), hh = __hmul2(kk, a);
-                    h[e] = as_word(hh);
-                    m[e] = as_word(__hfma2(kk, as_bf2(w2[2 * q + (e >> 1)]), __hfma2(kk, a, __hneg2(hh))));
-                }
-                tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 8 * q, h);
-                tmem_st_16x8(to + ((uint32_t)(16 * g) << 16) + 64 + 8 * q, m);
+            for (int e = 0; e < 8; ++e) {
+                const __nv_bfloat162 kk = as_bf2(k[e >> 2][g][e & 3]), a = as_bf2(w1[e >> 1]), hh = __hmul2(kk, a);
+                h[e] = as_word(hh);
+                m[e] = as_word(__hfma2(kk, as_bf2(w2[e >> 1]), __hfma2(kk, a, __hneg2(hh))));
             }
+            tmem_st_16x16(to + ((uint32_t)(16 * g) << 16), h);
+            tmem_st_16x16(to + ((uint32_t)(16 * g) << 16) + 64, m);
+        }
     }
 }
 // The third piece, what the first two leave of k w in fp32, back to where K was
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     const uint32_t s_smem = smem_u32(base), ring = s_smem + L::S_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, quad = warp & 3, lane = tid & 31, row = tid & 127;
     if (tid == 0) {
-        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.staged[i], 4); }
+        for (int i = 0; i < L::STAGES; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.q_full[i], 1); mbar_init(&sh.empty[i], 1); mbar_init(&sh.staged[i], 4); }
         for (int i = 0; i < RING; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.heard[i], ROLE_WARPS); }
         mbar_init(&sh.sc_full, 1); mbar_init(&sh.qs_done, 1); mbar_init(&sh.u_full, 1); mbar_init(&sh.o_full, 1);
         mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.low_ready, 8); mbar_init(&sh.s_ready, 8);
@@ -411,26 +411,27 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             for (int c = w.c0; c < w.c1 && on; ++c) {
                 const int t = w.step(c);
                 const uint32_t at = ring + (uint32_t)stage * L::STAGE;
-                auto load = [&](int r, uint32_t to, int width) {
+                auto load = [&](int r, uint32_t to, int width, uint64_t *bar) {
                     const int m = p.which[w.job][r], hh = p.flat[m] & 2 ? 0 : w.h, bb = p.flat[m] & 1 ? 0 : w.b;
 #pragma unroll 1
-                    for (int d = 0; d < width; d += 64) tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], &sh.full[stage], d, t, hh, bb);
+                    for (int d = 0; d < width; d += 64) tma_load_4d(to + (uint32_t)(d / 64) * (C * 128), &p.map[m], bar, d, t, hh, bb);
                 };
                 // Q's place (and K's, where the output is wider than Q) is given back later: the output goes out by way of it
                 on = warp_wait(sh, &sh.empty[stage], par);
                 if (!on) break;
                 if (elect_one()) {
-                    mbar_expect_tx(&sh.full[stage], L::STAGE);
-                    load(2, at + L::V, DV);
-                    if (DV <= DK) load(1, at + L::K, DK);
+                    mbar_expect_tx(&sh.full[stage], L::STAGE - C * DK * 2);
+                    if (DV <= DK) load(1, at + L::K, DK, &sh.full[stage]);
+                    load(2, at + L::V, DV, &sh.full[stage]);
                 }
                 __syncwarp();
                 if (loads >= L::STAGES) send(stage, par);
                 if (!on) break;
                 if (elect_one()) {
                     sh.out[stage] = Out{w.job, w.h, w.b, t, w.rows(c)};
-                    if (DV > DK) load(1, at + L::K, DK);
-                    load(0, at + L::Q, DK);
+                    if (DV > DK) load(1, at + L::K, DK, &sh.full[stage]);
+                    mbar_expect_tx(&sh.q_full[stage], C * DK * 2);
+                    load(0, at + L::Q, DK, &sh.q_full[stage]);
                 }
                 __syncwarp();
                 ++loads;
@@ -478,6 +479,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     for (int k = 0; k < C / 16; ++k) umma_ts(tmu + d, tmu + a + 8 * k, vd + k * K16, iv, add || k > 0);
                 };
                 wait(&sh.full[stage], full_par);
+                wait(&sh.q_full[stage], full_par);
                 if (on && elect_one()) {
                     const uint64_t kd = smem_desc_sw128(at + L::K);
 #pragma unroll 2
