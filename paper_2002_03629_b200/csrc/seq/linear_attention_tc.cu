@@ -167,6 +167,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
                    "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+                   "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -218,20 +226,35 @@ __device__ __forceinline__ void tmem_arrive(uint64_t *bar)
 // 128-byte swizzled tile: rows of 64 bf16; operand with N together ("MN-major"), panels of 64 columns `panel` bytes apart
 __device__ __forceinline__ uint64_t desc_mn(uint32_t at, uint32_t panel) { return smem_desc_sw128(at) + ((uint64_t)((panel >> 4) - 1) << 16); }
 
-// Sixteen words of P from 32 scores: times the columns' weights; columns not in `keep` are zero, whatever they hold
-__device__ __forceinline__ void p_pack(uint32_t (&s)[32], uint32_t (&w)[16], const float *weights, uint32_t keep)
+// 32 scores times their columns' weights
+__device__ __forceinline__ void p_weigh(uint32_t (&s)[32], const float *weights)
 {
 #pragma unroll
     for (int e = 0; e < 32; e += 4) {
         ulonglong2 r = *reinterpret_cast<const ulonglong2 *>(weights + e);
         r.x = mul2(r.x, pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
         r.y = mul2(r.y, pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])));
-        w[e / 2] = narrow(r.x);
-        w[e / 2 + 1] = narrow(r.y);
+        s[e] = (uint32_t)r.x;
+        s[e + 1] = (uint32_t)(r.x >> 32);
+        s[e + 2] = (uint32_t)r.y;
+        s[e + 3] = (uint32_t)(r.y >> 32);
     }
-    if (keep != 0xffffffffu)                                 // (the row's own block, and the last ones of a ragged chunk)
+}
+// Sixteen words of P from 32 values; columns not in `keep` are zero, whatever they hold
+__device__ __forceinline__ void p_words(const uint32_t (&s)[32], uint32_t (&w)[16], uint32_t keep)
+{
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] &= (keep >> (2 * e) & 1u ? 0xffffu : 0u) | (keep >> (2 * e + 1) & 1u ? 0xffff0000u : 0u);
+    for (int e = 0; e < 16; ++e) w[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+    if (!__any_sync(0xffffffffu, keep)) {                    // beyond the diagonal
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = 0;
+    } else if (keep != 0xffffffffu)                          // (the row's own block, and a ragged chunk)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            uint32_t m;                                      // bits 2 e and 2 e + 1 of `keep`, sixteen times each: signs of bytes 1 and 7, repeated
+            asm("prmt.b32 %0, %1, %2, 0xff99;" : "=r"(m) : "r"(2 * e < 15 ? keep << (15 - 2 * e) : keep >> (2 * e - 15)), "r"(keep << (30 - 2 * e)));
+            w[e] &= m;
+        }
 }
 
 // Weights of K's rows: lambda^(steps to the chunk's end) in time's direction, 0 behind the sequence's end
@@ -345,7 +368,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
         for (int i = 0; i < RING; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.heard[i], ROLE_WARPS); }
         mbar_init(&sh.sc_full, 1); mbar_init(&sh.qs_done, 1); mbar_init(&sh.u_full, 1); mbar_init(&sh.o_full, 1);
         mbar_init(&sh.p_ready, 4); mbar_init(&sh.k_ready, 8); mbar_init(&sh.low_ready, 8); mbar_init(&sh.s_ready, 8);
-        mbar_init(&sh.u_free, 8); mbar_init(&sh.o_scaled, 4); mbar_init(&sh.o_free, 4);
+        mbar_init(&sh.u_free, 8); mbar_init(&sh.o_scaled, 8); mbar_init(&sh.o_free, 4);
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -540,7 +563,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
         }
     } else if (warp < 4) {
         // ------------------------------------------------------------- O of the chunk before, and P
-        uint32_t par = 0, qs_par = 0;
+        uint32_t par = 0;
         bool on = true, more = true, due = false;
         Place place;
         Work w{};
@@ -602,7 +625,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             }
             const bool have = c < w.c1 && more;
             if (have) {
-                const bool back = w.flags & BACK, weak = w.flags & WEAK, state = w.state(c);
+                const bool back = w.flags & BACK, weak = w.flags & WEAK;
                 const int rows = w.rows(c), late = w.late(c);
                 if (on) on = warp_wait(sh, &sh.sc_full, par);
                 if (on) {
@@ -612,7 +635,12 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                         if (weak) {
 #pragma unroll 1
                             for (int j = lane; j < C; j += 32) sh.wp[j] = w.sum_scale * power_of(w.ld, MID - (back ? rows - 1 - j : j) - late);
-                        } else sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
+                        } else {
+                            sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
+                            const float own = w.sum_scale * la_power(w.ld, lane);  // 64 + d: d steps later (back: earlier); the other way there is nothing
+                            sh.wp[64 + lane] = back && lane > 0 ? 0.0f : own;
+                            sh.wp[64 - lane] = !back && lane > 0 ? 0.0f : own;
+                        }
                         __syncwarp();
                     }
                     // Columns of block b that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
@@ -628,15 +656,16 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                             tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
                             tmem_ld32_issue(lanes + COL_SC + 32 * b + 32, t);
                             tmem_wait_ld();
-                            p_pack(s, words, sh.wp + 32 * b, kept(b));
+                            p_weigh(s, sh.wp + 32 * b);
+                            p_words(s, words, kept(b));
                             tmem_st16(lanes + COL_SC + 16 * b, words);
-                            p_pack(t, words, sh.wp + 32 * b + 32, kept(b + 1));
+                            p_weigh(t, sh.wp + 32 * b + 32);
+                            p_words(t, words, kept(b + 1));
                             tmem_st16(lanes + COL_SC + 16 * b + 16, words);
                         }
                     } else {
 #pragma unroll 1
                         for (int b = 0; b < 4; ++b) {
-                            const uint32_t keep = kept(b);
                             uint32_t s[32], words[16];
                             tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
                             tmem_wait_ld();
@@ -645,41 +674,19 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                                 const float f = (back ? b > quad : b < quad) ? la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31) : 0.0f;
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
-                                p_pack(s, words, sh.wp, keep);
+                                p_weigh(s, sh.wp);
                             } else {
                                 // the row's own block: the power of the distance
+                                const float *const own = sh.wp + 64 + lane;
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const int far = max(back ? e - lane : lane - e, 0);
-                                    s[e] = keep >> e & 1u ? __float_as_uint(__uint_as_float(s[e]) * sh.wp[back ? far : 31 - far]) : 0u;
-                                }
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) words[e] = pack_bf16x2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+                                for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * own[-e]);
                             }
+                            p_words(s, words, kept(b));
                             tmem_st16(lanes + COL_SC + 16 * b, words);
                         }
                     }
                     tmem_wait_st();
                     tmem_arrive(&sh.p_ready);
-                }
-                if (state && !weak) {
-                    if (on) on = warp_wait(sh, &sh.qs_done, qs_par);
-                    qs_par ^= 1u;
-                    if (on) {
-                        const float g = row < rows ? la_power(w.ld, (back ? rows - 1 - row : row) + late) : 0.0f;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int v = 0; v < p.job[w.job].Dv; v += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(lanes + COL_O + v, r);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
-                            tmem_st16(lanes + COL_O + v, r);
-                        }
-                        tmem_wait_st();
-                        tmem_arrive(&sh.o_scaled);
-                    }
                 }
             }
             if (!have) break;
@@ -698,7 +705,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     } else {
         // ------------------------------------------------------------- K and S
         int stage = 0;
-        uint32_t full_par = 0, par = 0;
+        uint32_t full_par = 0, par = 0, qs_par = 0;
         bool on = true;
         const int half = (warp - 4) >> 2;                                          // of a chunk's steps and of the state's columns
         constexpr int HV = DV / 2, HC = C / 2;
@@ -792,6 +799,24 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.s_ready);
+                    if (!(w.flags & WEAK)) {                                       // Q S times lambda^(i+1), a row a thread, while the scores become P
+                        on = warp_wait(sh, &sh.qs_done, qs_par);
+                        qs_par ^= 1u;
+                        if (!on) break;
+                        tc_fence_after();
+                        const float g = row < rows ? la_power(w.ld, (w.flags & BACK ? rows - 1 - row : row) + w.late(c)) : 0.0f;
+#pragma unroll 1
+                        for (int v = v0; v < min(v0 + HV, Dv); v += 32) {          // (columns beyond Dv hold something or other)
+                            uint32_t r[32];
+                            tmem_ld32_issue(lanes + COL_O + v, r);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
+                            tmem_st32(lanes + COL_O + v, r);
+                        }
+                        tmem_wait_st();
+                        tmem_arrive(&sh.o_scaled);
+                    }
                 }
                 on = warp_wait(sh, &sh.u_full, par);
                 par ^= 1u;
