@@ -8,16 +8,17 @@
 // Packed sequences: a kernel of one CTA sorts them by length, and the CTAs take the next unit as they come free.
 // Roles:
 //   P, O  four warps: scores from tensor memory, masked and decayed, as bf16 back over them (the left operand of P V); then the chunk before's
-//         outputs to memory.  Under strong decay Q S is scaled by lambda^(i+1) in tensor memory before P V is added.
+//         outputs to memory.
 //   K, S  eight warps: K from shared memory, transposed on the way, weighted and cut into two or three bf16 pieces (the left operand of
 //         U; one piece would leave the fp32 state off by 2e-3, three leave 5e-7; two, off by 3e-6, do where nobody asks for the state): two into
 //         tensor memory, the third back to where K was.  The state, fp32, in registers, a row of Dv / 2 values a thread; rounded to bf16 into shared
-//         memory for Q S.
+//         memory for Q S.  Under strong decay they scale Q S by lambda^(i+1) in tensor memory before P V is added.  (They have the time: with the
+//         outputs as their work too, gradients of 8 x 2048 steps took 204 to 220 us, a prompt of 65536 steps 323 to 336.)
 //   a warp that finds units and loads tiles (TMA, a ring of stages that runs on across chunks and units), one that issues the MMAs
-// Bound: the chain of the roles from one chunk to the next, 4.2 us a chunk and SM at widths of 128 (tensor pipe active for 28 % of the time, issue slots
-// for 35 %, DRAM for 30 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
-// Measured, bf16, 16 heads of 128: one prompt of 65536 steps 340 us (own states 83, their chain 10, outputs 245; 1.07 GB, 3.2 TB/s); gradients of 8 x 2048
-// steps 214 us; 20 packed prompts of 1 to 2500 steps 102 us (196 with the units dealt out beforehand).
+// Bound: the chain of the roles from one chunk to the next, 4 us a chunk and SM at widths of 128 (tensor pipe active for 30 % of the time, issue slots
+// for 35 %, DRAM for 32 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
+// Measured, bf16, 16 heads of 128: one prompt of 65536 steps 335 us (own states 81, their chain 9, outputs 245; 1.07 GB, 3.2 TB/s); gradients of 8 x 2048
+// steps 204 us; 20 packed prompts of 1 to 2500 steps 97 us (196 with the units dealt out beforehand).
 // Tensor memory is full: scores and P over them, U, O and K's pieces take 128 columns each.
 // The roles' loops are kept short and free of what can be done once: unrolled further, or with the search for units in each of them, their code
 // fell out of the instruction cache.  setmaxnreg for one role with a whole row of the state a thread was slower (20 warps, spills in others).
