@@ -16,13 +16,14 @@
  * steps.  With it (int32 [N + 1] on the device, ascending from 0 or more to at most T) B is 1 and sequence i takes the steps
  * cu_seqlens[i] .. cu_seqlens[i + 1] - 1; steps that no sequence takes are neither read nor written.  (What the device finds
  * outside [0, T] or descending is cut to that range: no memory outside is touched.)  States are fp32 [B or N][H][Dk][Dv], dense; a state that is
- * written may not overlap one that is read.
+ * written may not overlap one that is read; nor may any other result overlap an input or another result.
  *
  * Types: LA_F32 or LA_BF16 for q, k, v, o and their gradients; sums and states are fp32.  Where bf16 rows lie on 16 bytes (base and strides)
  * and Dk, Dv are multiples of 16, and in la_forward and la_backward only, the products take bf16 factors: the intermediate
  * scores and the state that a chunk starts from are rounded to bf16 before their product, the sums that a state is made of are not (its factors go in
  * two or three bf16 pieces: off by 3e-6 in the first case, which is taken where no state is asked for or the chunk is too far back to be seen in
- * it).  Everywhere else the products are of fp32 values in two pieces of 22 bits together.
+ * it).  Everywhere else the products are of fp32 values in two pieces of 22 bits together (fewer below 2^-104: what
+ * lies under 2^-136 is lost; magnitudes from 3.402e38 on count as infinite).
  * Values that are not finite: outputs of the chunk of up to 128 steps that holds one, and everything that depends on it, are not specified; no
  * other sequence and no other head is touched.
  *

@@ -123,7 +123,8 @@ def linear_attention(q, k, v, log_decay, scale: float = 1.0, state=None, cu_seql
 
     q, k [B,T,H,Dk], v [B,T,H,Dv] float32 or bfloat16, any strides with a head's values side by side; log_decay [H] float32;
     state [B,H,Dk,Dv] float32: the states to go on from (None: zeros).  cu_seqlens int32 [N+1]: packed sequences (B = 1,
-    states [N,H,Dk,Dv]); steps that belong to none of them are left as they are in `out` (undefined without it)."""
+    states [N,H,Dk,Dv]); steps that belong to none of them are left as they are in `out` (undefined without it), which shares no
+    memory with the inputs."""
     s, n, index = _shape(q, v, log_decay, scale, cu_seqlens)
     if _elsewhere(index, stream):
         with _there(index, stream):

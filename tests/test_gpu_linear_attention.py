@@ -4,6 +4,8 @@ Tolerance.  With M the same recurrence of the magnitudes |q|, |k|, |v|, |S0| (ev
 lambda^n > 0), an fp32 computation whose longest chain of additions has c terms is off by at most (c + 16) u M, u = 2^-24: a product, a
 weight (an exponential of 2 ulp of an argument rounded once, n |log lambda| <= 90 where it counts: below 8 u for the weights that matter) and c additions.  Chains: Dk
 terms of a score, at most 128 steps of a chunk, then one addition for every chunk and two roundings of the state: c = Dk + 128 + 3 n / 32.
+Products of fp32 factors in two TF32 pieces are off by 3 * 2^-22 = 12 u each, two of them in a row by 24 u, and sums that are cut towards zero by 2 u an
+addition, of eight terms at a time: with chunks of 32 steps Dk / 4 + 8 of them, in all 24 + Dk / 4 + 8 < Dk + 128.
 bf16 outputs are rounded by eps / 2 of themselves; on the tensor cores the scores and the state at the chunk's start are rounded to
 bf16 before their product, each by eps / 2 of its magnitude, below eps / 2 M together."""
 import numpy as np
@@ -333,6 +335,74 @@ def test_captured_replayed_and_on_two_streams(dtype):
     other = la.linear_attention(d["q"], d["k"], d["v"], d["ld"], state=d["state"], stream=s)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(other, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("decays", [[-0.01, -0.3], [-2.0, -0.9]], ids=["weak", "strong"])
+def test_what_is_not_finite_stays_in_its_sequence_and_head(decays, dtype):
+    """NaN, infinities and the types' largest values in one sequence, then in one head: all the others keep their bits."""
+    from paper_2002_03629_b200 import linear_attention as la
+    lens = [130, 45, 300, 7]
+    at = np.concatenate([[0], np.cumsum(lens)])
+    x = make(1, sum(lens), 2, 64, 64, dtype, seed=8, decays=decays, state=False)
+    g = torch.Generator().manual_seed(5)
+    x["state"], x["dstate"] = (torch.randn(4, 2, 64, 64, generator=g) for _ in range(2))
+    cu = torch.tensor(at, dtype=torch.int32).cuda()
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max, torch.finfo(dtype).min, 1.0]).to(dtype)
+
+    def run(y):
+        d = dev(y)
+        return (*la.linear_attention(d["q"], d["k"], d["v"], d["ld"], scale=0.1, state=d["state"], cu_seqlens=cu),
+                *la.linear_attention_backward(d["q"], d["k"], d["v"], d["ld"], d["do"], scale=0.1, state=d["state"], dstate=d["dstate"], cu_seqlens=cu))
+    want = run(x)
+    for part in (1, 2):
+        y = {a: t.clone() for a, t in x.items()}
+        for a in ("q", "k", "v", "do"):
+            y[a][:, at[part]:at[part + 1]] = bad[torch.randint(0, 6, y[a][:, at[part]:at[part + 1]].shape, generator=g)]
+        for a, b in zip(run(y), want):
+            rows = [i for i in range(4) if i != part]
+            if a.shape[0] == 4:
+                assert torch.equal(a[rows], b[rows])
+            else:
+                for i in rows:
+                    assert torch.equal(a[:, at[i]:at[i + 1]], b[:, at[i]:at[i + 1]])
+    y = {a: t.clone() for a, t in x.items()}
+    for a in ("q", "k", "v", "do"):
+        y[a][:, :, 0] = bad[torch.randint(0, 6, y[a][:, :, 0].shape, generator=g)]
+    for a, b in zip(run(y), want):
+        assert torch.equal(a[:, 1], b[:, 1]) if a.shape[0] == 4 else torch.equal(a[:, :, 1], b[:, :, 1])
+
+
+@pytest.mark.parametrize("heads", [2, 40])
+def test_packed_sequences_replayed_on_two_streams(heads):
+    """The counter that the units are taken by, and the order of the segments, belong to the call: graphs and an eager call side by side, the same bits."""
+    from paper_2002_03629_b200 import linear_attention as la
+    lens = [1500, 3, 0, 700, 129, 1024, 64]
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32).cuda()
+    d = dev(make(1, sum(lens), heads, 64, 64, torch.bfloat16, seed=6, state=False, decays=[-0.02] * heads))
+
+    def call():
+        return (*la.linear_attention(d["q"], d["k"], d["v"], d["ld"], cu_seqlens=cu),
+                *la.linear_attention_backward(d["q"], d["k"], d["v"], d["ld"], d["do"], cu_seqlens=cu))
+    want = call()
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call())
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        with torch.cuda.stream(streams[2]):
+            eager = call()
+    torch.cuda.synchronize()
+    for o in (*outs, eager):
+        assert all(torch.equal(a, b) for a, b in zip(o, want))
 
 
 def test_gradient_against_differences():
