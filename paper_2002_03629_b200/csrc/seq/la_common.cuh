@@ -37,6 +37,8 @@ __device__ __forceinline__ int la_sequence(const LaSeqs &s, int seq, long long &
     start = a;
     return (int)(b - a);
 }
+// The slot of a packed sequence's first segment (of `seg` steps): it owns at least as many as it has segments
+__device__ __forceinline__ int la_first_slot(const LaSeqs &seqs, int seg, int seq) { return min(max(__ldg(seqs.cu + seq), 0), (int)seqs.T) / seg + seq; }
 // lambda^n; n = 0 is 1 whatever lambda
 __device__ __forceinline__ float la_power(float log_decay, int n) { return n == 0 ? 1.0f : expf((float)n * log_decay); }
 

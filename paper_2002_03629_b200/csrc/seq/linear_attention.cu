@@ -1,6 +1,7 @@
 // Linear attention with a decay for each head (formulas: include/linear_attention.h): entry points, single steps, and the kernel that takes
 // every type, size and stride.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdio>
 
@@ -28,7 +29,7 @@ int status(cudaError_t e)
 // registers cost two CTAs an SM: 168 us in place of 159.
 // Measured: gradients of 592 x 100 steps, 4 heads of 32, fp32: 159 us (multiply-adds 221; 454 MB at least, 2.9 TB/s); one prompt of 100 steps, 8 heads
 // of 64: 13.5 us, the latency of four chunks after one another.
-constexpr int CH = 32;
+constexpr int CH = 32, C128 = 128;           // segments are whole multiples of 128 steps
 
 template <int DK, int VS, int G>
 struct AnyTiles {
@@ -105,9 +106,13 @@ __device__ __forceinline__ bool la_groups(const T *p, long long token, int width
     return width % N == 0 && ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(token * (long long)sizeof(T))) & (N * sizeof(T) - 1)) == 0;
 }
 
-template <typename T, int DK, int VS, int G>
-__global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs)
+// CUT: the sequences are cut into segments; `only` then asks for the segments' own states, from zero, and no outputs.  (Kernels of their own: the
+// same code with the choice made as it runs took 176 us for 159.)
+template <typename T, int DK, int VS, int G, bool CUT>
+__global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs,
+                                                                                    const __grid_constant__ LaCut cut, bool only)
 {
+    const bool states = CUT && only;
     using L = AnyTiles<DK, VS, G>;
     extern __shared__ __align__(16) float sm[];
     const LaJob &job = jobs.job[blockIdx.z];
@@ -115,16 +120,30 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
     if (c0 >= job.Dv) return;
     float *const q = sm, *const k = q + CH * L::QW, *const v = k + CH * L::QW, *const St = v + CH * L::VW, *const A = St + DK * L::SW,
           *const pw = A + CH * L::AW, *const wk = pw + CH + 4;           // pw[n] = lambda^n, n <= CH; weights of K's rows
-    const int cols = min(VS, job.Dv - c0), seq = blockIdx.x / seqs.H, h = blockIdx.x % seqs.H;
+    const int cols = min(VS, job.Dv - c0), h = blockIdx.x % seqs.H;
+    int seq = blockIdx.x / seqs.H, slot = seq, part = 0;                       // of a sequence's segments
+    if constexpr (CUT) {
+        if (seqs.cu == nullptr) {
+            seq = slot / cut.per;
+            part = slot % cut.per;
+        } else {
+            if (slot >= cut.next[states ? 2 : 1]) return;
+            seq = cut.order[slot].x;
+            part = cut.order[slot].y;
+            slot = la_first_slot(seqs, cut.seg, seq) + part;
+        }
+    }
     long long start;
-    const int n = la_sequence(seqs, seq, start);
+    const int n = la_sequence(seqs, seq, start), begin = CUT ? part * cut.seg : 0, end = CUT ? (int)min((long long)begin + cut.seg, (long long)n) : n;
+    if (states && end == n) return;                                            // the last segment's own state is not wanted
     const float ld = seqs.log_decay[h];
     const int b = seqs.cu == nullptr ? seq : 0;
     const T *const qg = (const T *)job.q.data + b * job.q.batch + start * job.q.token + h * job.q.head;
     const T *const kg = (const T *)job.k.data + b * job.k.batch + start * job.k.token + h * job.k.head;
     const T *const vg = (const T *)job.v.data + b * job.v.batch + start * job.v.token + h * job.v.head + c0;
     T *const og = (T *)job.o.data + b * job.o.batch + start * job.o.token + h * job.o.head + c0;
-    const size_t sbase = (size_t)blockIdx.x * Dk * job.Dv;
+    const size_t sbase = ((size_t)seq * seqs.H + h) * Dk * job.Dv;
+    float *const carry = CUT ? cut.carry + (((size_t)blockIdx.z * cut.slots + slot) * seqs.H + h) * Dk * job.Dv + c0 : nullptr;
     for (int p = tid; p <= CH; p += G) pw[p] = la_power(ld, p);
     // this thread's place in a fragment; the warp's rows of a chunk, and its columns of the scores and outputs; its rows of the state
     const int warp = tid / 32, g = tid / 4 % 8, t = tid % 4;
@@ -135,8 +154,10 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int d = d0 + x / 2 * 8, e = 8 * b + 2 * t + x % 2;
-            S[b][x] = job.s0 != nullptr && d < Dk && e < cols
-                          ? job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)] : 0.0f;
+            S[b][x] = 0.0f;
+            if (states || d >= Dk || e >= cols) continue;
+            if (CUT && part > 0) S[b][x] = carry[(size_t)d * job.Dv + e];
+            else if (job.s0 != nullptr) S[b][x] = job.s0[sbase + (job.turned ? (size_t)(c0 + e) * Dk + d : (size_t)d * job.Dv + c0 + e)];
         }
     // a chunk's rows, by way of registers: thread = four columns and every eighth (V: RV-th) step
     constexpr int RQ = 4 * G / DK, RV = 4 * G / VS;
@@ -151,17 +172,17 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
         const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int p = 0; p < L::NQ; ++p, pq += sq, pk += sk) {
-            const bool in = t0 + qi + p * RQ < n && qd < Dk;
-            rq[p] = in ? la_four(pq, Dk - qd, q4) : zero;
+            const bool in = t0 + qi + p * RQ < end && qd < Dk;
+            rq[p] = in && !states ? la_four(pq, Dk - qd, q4) : zero;
             rk[p] = in ? la_four(pk, Dk - qd, q4) : zero;
         }
 #pragma unroll
-        for (int p = 0; p < L::NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < n && vc < cols ? la_four(pv, cols - vc, v4) : zero;
+        for (int p = 0; p < L::NV; ++p, pv += sv) rv[p] = t0 + vi + p * RV < end && vc < cols ? la_four(pv, cols - vc, v4) : zero;
     };
-    int late = job.back ? 0 : 1;
+    int late = job.back && begin == 0 ? 0 : 1;
 #pragma unroll 1
-    for (int t0 = 0; t0 < n; t0 += CH, late = 1) {
-        const int rows = min(CH, n - t0);
+    for (int t0 = begin; t0 < end; t0 += CH, late = 1) {
+        const int rows = min(CH, end - t0);
         fetch(t0);
         __syncthreads();                                     // the chunk before is done with
 #pragma unroll
@@ -171,6 +192,7 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
         }
 #pragma unroll
         for (int p = 0; p < L::NV; ++p) *reinterpret_cast<float4 *>(v + (vi + p * RV) * L::VW + vc) = rv[p];
+        if (!states)
 #pragma unroll
         for (int b = 0; b < L::SN; ++b) {
             *reinterpret_cast<float2 *>(St + d0 * L::SW + 8 * b + 2 * t) = make_float2(S[b][0], S[b][1]);
@@ -182,7 +204,7 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
             const float2 a = *reinterpret_cast<const float2 *>(q + i0 * L::QW + at + 2 * t), b = *reinterpret_cast<const float2 *>(q + (i0 + 8) * L::QW + at + 2 * t);
             x[0] = a.x; x[1] = b.x; x[2] = a.y; x[3] = b.y;
         };
-        if (row0 < rows) {
+        if (row0 < rows && !states) {
             float acc[L::AN][4] = {};
             if (ac < row0 + 16)                              // (else above the diagonal)
                 multiply<L::AN>(acc, DK, q_rows, [&](int at, int b, float (&y)[2]) {
@@ -198,8 +220,8 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
                                                                                  j < i && i < rows ? acc[b][2 * x + 1] * (job.sum_scale * pw[i - j - 1]) : 0.0f);
                 }
         }
-        __syncthreads();
-        if (row0 < rows) {
+        if (!states) __syncthreads();
+        if (row0 < rows && !states) {
             float o[L::ON][4] = {};
             multiply<L::ON>(o, DK, q_rows, [&](int at, int b, float (&y)[2]) {
                 const float *const x = St + (at + 2 * t) * L::SW + oc + 8 * b + g;
@@ -257,14 +279,15 @@ __global__ void __launch_bounds__(G, DK == 32 ? 8 : DK == 64 ? 3 : 2) la_any_ker
                 for (int x = 0; x < 4; ++x) S[b0 + b][x] = step(S[b0 + b][x], U[b][x]);
         }
     }
-    if (job.s1 == nullptr) return;
-    const float last = job.back && n > 0 ? la_power(ld, 1) : 1.0f;
+    float *const to = states ? carry : end == n && job.s1 != nullptr ? job.s1 + sbase + c0 : nullptr;
+    if (to == nullptr) return;
+    const float last = job.back && n > 0 && !states ? la_power(ld, 1) : 1.0f;
 #pragma unroll
     for (int b = 0; b < L::SN; ++b)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int d = d0 + x / 2 * 8, e = 8 * b + 2 * t + x % 2;
-            if (d < Dk && e < cols) job.s1[sbase + (size_t)d * job.Dv + c0 + e] = last * S[b][x];
+            if (d < Dk && e < cols) to[(size_t)d * job.Dv + e] = last * S[b][x];
         }
 }
 
@@ -351,28 +374,58 @@ bool tensor_ok(const la_shape *s, const la_tensor *t, long long rows)
     return t->data != nullptr && (reinterpret_cast<uintptr_t>(t->data) & (s->type == LA_F32 ? 3u : 1u)) == 0;
 }
 
-template <typename T, int DK, int VS, int G>
-cudaError_t launch_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dv, cudaStream_t stream)
+// Segments of sequences where there is room for more CTAs than sequences and heads give.  Time in chunks of one CTA alone on its SM: with c of them each
+// takes 0.55 c times as long; half of the columns each (few sequences and heads, not cut), three quarters; the pass for the segments' own states takes
+// two fifths of the other's time, its launches and the chain between them that of eight chunks.  (fp32, one prompt, heads of 64: 16384 steps, 4 heads
+// 1544 us uncut, 94 cut; 1000 steps, 8 heads 99 and 68; 500 steps 54 and 68.)  Packed: none of more than twice a CTA's share.
+LaPlan any_plan(const la_shape *s, int jobs)
 {
-    auto kernel = la_any_kernel<T, DK, VS, G>;
-    constexpr size_t smem = AnyTiles<DK, VS, G>::FLOATS * sizeof(float);
-    if constexpr (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
+    const long long n = s->cu_seqlens != nullptr ? s->N : s->B, sms = la_sms(), widest = std::max(s->Dk, s->Dv);
+    const long long heads = std::max(1ll, n * s->H * jobs), ctas = heads * ((widest + 63) / 64), share = 2 * sms;
+    const long long steps = s->cu_seqlens != nullptr ? (n > 0 ? (s->T + n - 1) / n : 0) : s->T, units = (steps + C128 - 1) / C128;
+    auto slower = [&](long long c) { return std::max(1.0, 0.55 * (double)((c + sms - 1) / sms)); };
+    long long best = std::max(1ll, (s->T + C128 - 1) / C128);
+    double cost = (double)(units * (C128 / CH)) * slower(ctas) * (heads * 2 <= sms && widest <= 64 ? 0.75 : 1.0);
+    for (long long parts = 2; parts <= 128 && 2 * parts <= units; ++parts) {
+        const long long per = (units + parts - 1) / parts;
+        const double c = (double)(per * (C128 / CH)) * slower(ctas * parts) * 1.4 + 8.0;
+        if (c < cost) { cost = c; best = per; }
     }
-    kernel<<<dim3((unsigned)(seqs.n * seqs.H), (dv + VS - 1) / VS, count), G, smem, stream>>>(jobs, seqs);
-    return cudaGetLastError();
+    if (s->cu_seqlens != nullptr && n > 1) best = std::min(best, std::max(4ll, 2 * ((s->T / C128 + n) * s->H * jobs * ((widest + 63) / 64) / share + 1)));
+    LaPlan plan{};
+    la_plan_slots(plan, s, jobs, best);
+    if (plan.fits && plan.slots <= n) plan.bytes = 0;        // (nothing is cut: no order either)
+    return plan;
+}
+
+template <typename T, int DK, int VS, int G>
+cudaError_t launch_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dv, const LaCut &cut, int size, cudaStream_t stream)
+{
+    constexpr size_t smem = AnyTiles<DK, VS, G>::FLOATS * sizeof(float);
+    auto launch = [&](auto kernel, int slots, bool only) {
+        cudaError_t e = cudaSuccess;
+        if constexpr (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        kernel<<<dim3((unsigned)(slots * seqs.H), (dv + VS - 1) / VS, count), G, smem, stream>>>(jobs, seqs, cut, only);
+        return cudaGetLastError();
+    };
+    if (cut.carry == nullptr) return launch(la_any_kernel<T, DK, VS, G, false>, seqs.n, false);
+    cudaError_t e = seqs.cu != nullptr ? la_order(seqs, cut, 0, stream) : cudaSuccess;
+    if (e == cudaSuccess) e = launch(la_any_kernel<T, DK, VS, G, true>, cut.slots, true);
+    if (e == cudaSuccess) e = la_carry(jobs, count, seqs, cut, size, stream);
+    return e == cudaSuccess ? launch(la_any_kernel<T, DK, VS, G, true>, cut.slots, false) : e;
 }
 // Widths up to 32, 64, 128; at 128 the state's columns are shared by two CTAs, each of which computes the scores
 template <typename T>
-cudaError_t run_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dk, int dv, cudaStream_t stream)
+cudaError_t run_any(const LaJobs &jobs, const LaSeqs &seqs, int count, int dk, int dv, const LaCut &cut, int size, cudaStream_t stream)
 {
-    if (dk <= 32) return launch_any<T, 32, 32, 64>(jobs, seqs, count, dv, stream);
+    if (dk <= 32) return launch_any<T, 32, 32, 64>(jobs, seqs, count, dv, cut, size, stream);
     // (few sequences and heads: two CTAs a head, a half of the state's columns each, while all of them have an SM of their own; one prompt of 100 steps,
     // 8 heads of 64: 13.5 us for 19)
-    const bool few = (long long)seqs.n * seqs.H * count * 2 <= 148;
-    if (dk <= 64) return dv <= 32 || few ? launch_any<T, 64, 32, 128>(jobs, seqs, count, dv, stream) : launch_any<T, 64, 64, 128>(jobs, seqs, count, dv, stream);
-    return launch_any<T, 128, 64, 256>(jobs, seqs, count, dv, stream);
+    const bool few = cut.carry == nullptr && (long long)seqs.n * seqs.H * count * 2 <= la_sms();
+    if (dk <= 64) return dv <= 32 || few ? launch_any<T, 64, 32, 128>(jobs, seqs, count, dv, cut, size, stream)
+                                         : launch_any<T, 64, 64, 128>(jobs, seqs, count, dv, cut, size, stream);
+    return launch_any<T, 128, 64, 256>(jobs, seqs, count, dv, cut, size, stream);
 }
 
 int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const *tensors, int n_in, int n_all, const int (*which)[3], void *workspace,
@@ -380,7 +433,8 @@ int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const
 {
     const LaSeqs seqs{s->cu_seqlens != nullptr ? s->N : s->B, s->H, s->T, s->cu_seqlens, s->log_decay};
     if (seqs.n == 0) return LA_OK;
-    bool aligned = (reinterpret_cast<uintptr_t>(workspace) & 15u) == 0;
+    const bool room = (reinterpret_cast<uintptr_t>(workspace) & 15u) == 0;
+    bool aligned = room;
     for (int j = 0; j < count; ++j)
         aligned = aligned && ((reinterpret_cast<uintptr_t>(jobs.job[j].s0) | reinterpret_cast<uintptr_t>(jobs.job[j].s1)) & 15u) == 0;
     if (aligned && la_tc_takes(s, count, tensors, n_all)) return status(la_tc_run(s, jobs, count, tensors, n_in, which, workspace, stream));
@@ -389,18 +443,24 @@ int run(const la_shape *s, const LaJobs &jobs, int count, const la_tensor *const
         dk = std::max(dk, jobs.job[j].Dk);
         dv = std::max(dv, jobs.job[j].Dv);
     }
-    return status(s->type == LA_F32 ? run_any<float>(jobs, seqs, count, dk, dv, stream) : run_any<__nv_bfloat16>(jobs, seqs, count, dk, dv, stream));
+    const LaPlan plan = any_plan(s, count);
+    LaCut cut{INT_MAX, 0, 1, nullptr, nullptr, nullptr};     // (not cut)
+    if (room && plan.fits && plan.slots > seqs.n) cut = la_cut(plan, seqs.n, s->cu_seqlens != nullptr, workspace);
+    const int size = s->Dk * s->Dv;
+    return status(s->type == LA_F32 ? run_any<float>(jobs, seqs, count, dk, dv, cut, size, stream) : run_any<__nv_bfloat16>(jobs, seqs, count, dk, dv, cut, size, stream));
 }
 
 }  // namespace
 
 extern "C" {
 
-// (What the tensor-core path needs, taken or not: whether the tensors may go that way is seen with them.)
+// (Enough for either path: which one the tensors may take is seen with them.)
 size_t la_workspace(const la_shape *s, int backward)
 {
     if (!shape_ok(s)) return 0;
-    return std::max<size_t>(16, s->type == LA_BF16 && s->Dk % 16 == 0 && s->Dv % 16 == 0 ? la_tc_plan(s, backward ? 3 : 1).bytes : 0);
+    const int jobs = backward ? 3 : 1;
+    const size_t tc = s->type == LA_BF16 && s->Dk % 16 == 0 && s->Dv % 16 == 0 ? la_tc_plan(s, jobs).bytes : 0;
+    return std::max<size_t>({16, tc, any_plan(s, jobs).bytes});
 }
 
 int la_forward(const la_shape *s, const la_tensor *q, const la_tensor *k, const la_tensor *v, const float *state0, const la_tensor *o,

@@ -41,14 +41,8 @@ struct Params {
     int which[3][3];                         // a job's q, k, v: number of the tensor map
     int flat[4], out_flat[3];                // tensors whose batch (1) or head (2) stride is 0, or that have only one: coordinate 0
     LaSeqs seqs;
-    int jobs, slots, per;                    // slots: segments of all sequences; per: of one, where all are alike
-    int seg;                                 // steps of a segment, a multiple of C
-    int units;
-    float *carry;                            // [job][slot][head][Dk][Dv]
-    // packed sequences: the next unit to be taken, the number of segments, how many have others behind them; the segments (sequence, number in
-    // it), longest first, those with others behind them before all
-    int *next;
-    int2 *order;
+    int jobs, units;
+    LaCut cut;
 };
 
 struct Unit {
@@ -58,13 +52,11 @@ struct Unit {
     long long start;
 };
 
-// The slot of a packed sequence's first segment: it owns at least as many as it has segments
-__device__ __forceinline__ int first_slot(const LaSeqs &seqs, int seg, int seq) { return min(max(__ldg(seqs.cu + seq), 0), (int)seqs.T) / seg + seq; }
 // How many units there are (packed sequences: known to the device only)
-__device__ __forceinline__ int unit_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.next + 1) * p.seqs.H * p.jobs; }
+__device__ __forceinline__ int unit_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.cut.next + 1) * p.seqs.H * p.jobs; }
 
 // ... and how many may be of segments with others behind them
-__device__ __forceinline__ int cut_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.next + 2) * p.seqs.H * p.jobs; }
+__device__ __forceinline__ int cut_count(const Params &p) { return p.seqs.cu == nullptr ? p.units : __ldg(p.cut.next + 2) * p.seqs.H * p.jobs; }
 
 // Unit u
 __device__ __forceinline__ void get_unit(const Params &p, int u, Unit &x)
@@ -76,17 +68,17 @@ __device__ __forceinline__ void get_unit(const Params &p, int u, Unit &x)
     int s;
     if (p.seqs.cu == nullptr) {
         x.slot = u;
-        x.seq = u / p.per;
-        s = u % p.per;
+        x.seq = u / p.cut.per;
+        s = u % p.cut.per;
     } else {
-        const int2 e = __ldg(p.order + u);
+        const int2 e = __ldg(p.cut.order + u);
         x.seq = e.x;
         s = e.y;
-        x.slot = first_slot(p.seqs, p.seg, x.seq) + s;
+        x.slot = la_first_slot(p.seqs, p.cut.seg, x.seq) + s;
     }
     x.n = la_sequence(p.seqs, x.seq, x.start);
-    const long long at = (long long)s * p.seg;
-    const long long end = min(at + p.seg, (long long)x.n);
+    const long long at = (long long)s * p.cut.seg;
+    const long long end = min(at + p.cut.seg, (long long)x.n);
     x.c0 = (int)(at / C);
     x.c1 = (int)((end + C - 1) / C);
     x.last = end == x.n;
@@ -425,7 +417,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             w.ld = p.seqs.log_decay[x.h];
             w.sum_scale = job.sum_scale;
             w.last = job.back && x.n > 0 ? la_power(w.ld, 1) : 1.0f;
-            w.from = x.c0 > 0 ? p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * size : job.s0 != nullptr ? job.s0 + state : nullptr;
+            w.from = x.c0 > 0 ? p.cut.carry + (((size_t)x.job * p.cut.slots + x.slot) * p.seqs.H + x.h) * size : job.s0 != nullptr ? job.s0 + state : nullptr;
             w.to = x.last && job.s1 != nullptr ? job.s1 + state : nullptr;
             w.flags = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (w.ld >= -44.0f / MID ? WEAK : 0) | (w.from != nullptr ? INIT : 0) |
                       (x.c0 == 0 && job.turned ? TURNED : 0) | (end ? END : 0);
@@ -463,7 +455,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             }
             // Units of one length: every gridDim-th; of different ones: the next that nobody has
             if (p.seqs.cu == nullptr) u += gridDim.x;
-            else u = __shfl_sync(0xffffffffu, lane == 0 ? atomicAdd(p.next, 1) : 0, 0);
+            else u = __shfl_sync(0xffffffffu, lane == 0 ? atomicAdd(p.cut.next, 1) : 0, 0);
         }
         // the last outputs, oldest first
         if (loads < L::STAGES) stage = 0;                                          // (par is then that of no load: the first of `staged` is due)
@@ -1010,7 +1002,7 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
             const int Dk = job.Dk, Dv = job.Dv;
             if (row < Dk) {
                 const float f = on ? 1.0f : NAN;
-                float4 *const to = reinterpret_cast<float4 *>(p.carry + (((size_t)x.job * p.slots + x.slot) * p.seqs.H + x.h) * Dk * Dv + (size_t)row * Dv);
+                float4 *const to = reinterpret_cast<float4 *>(p.cut.carry + (((size_t)x.job * p.cut.slots + x.slot) * p.seqs.H + x.h) * Dk * Dv + (size_t)row * Dv);
 #pragma unroll
                 for (int v = 0; v < DV; v += 4)
                     if (v < Dv) to[v / 4] = make_float4(f * lo(S[v / 2]), f * hi(S[v / 2]), f * lo(S[v / 2 + 1]), f * hi(S[v / 2 + 1]));
@@ -1031,28 +1023,28 @@ __global__ void __launch_bounds__(STATE_TH, 1) la_state_kernel(const __grid_cons
 
 // They become the states that the segments start from: C_0 = S0, C_{i+1} = lambda^seg C_i + own_i.  A thread per value; the loads do not wait for
 // the sums (eight segments' worth in flight).
-__global__ void la_carry_kernel(LaJobs jobs, LaSeqs seqs, int slots, int per, int seg, const int *next, const int2 *order, float *carry)
+__global__ void la_carry_kernel(const __grid_constant__ LaJobs jobs, const __grid_constant__ LaSeqs seqs, const __grid_constant__ LaCut cut)
 {
-    const int job_i = blockIdx.z, h = blockIdx.x % seqs.H;
+    const int job_i = blockIdx.z, h = blockIdx.x % seqs.H, seg = cut.seg;
     int seq = blockIdx.x / seqs.H;
     const LaJob &job = jobs.job[job_i];
     const int e = blockIdx.y * blockDim.x + threadIdx.x, size = job.Dk * job.Dv;
     if (seqs.cu != nullptr) {                                // only sequences that are cut
-        if (seq >= next[2]) return;
-        const int2 s = order[seq];
+        if (seq >= cut.next[2]) return;
+        const int2 s = cut.order[seq];
         if (s.y != 0) return;
         seq = s.x;
     }
     if (e >= size) return;
     long long start;
     const int n = la_sequence(seqs, seq, start);
-    const int slot = seqs.cu == nullptr ? seq * per : first_slot(seqs, seg, seq);
+    const int slot = seqs.cu == nullptr ? seq * cut.per : la_first_slot(seqs, seg, seq);
     const int d = e / job.Dv, v = e % job.Dv, parts = (n + seg - 1) / seg;
     float S = 0.0f;
     if (job.s0 != nullptr) S = job.s0[((size_t)seq * seqs.H + h) * size + (job.turned ? (size_t)v * job.Dk + d : (size_t)e)];
     const float ld = seqs.log_decay[h];
     const LaStep step(ld, seg);
-    float *c = carry + (((size_t)job_i * slots + slot) * seqs.H + h) * size + e;
+    float *c = cut.carry + (((size_t)job_i * cut.slots + slot) * seqs.H + h) * size + e;
     const size_t step_on = (size_t)seqs.H * size;
     if (parts > 1) S = LaStep(ld, seg - (job.back ? 1 : 0))(S, *c);       // (the first segment starts from S0 itself)
     c += step_on;
@@ -1132,20 +1124,51 @@ cudaError_t launch(const Params &p, int dk, int dv, bool states, int sms, cudaSt
                     : (dv <= 64 ? launch<128, 64>(p, states, sms, stream) : launch<128, 128>(p, states, sms, stream));
 }
 
-int sm_count()
+}  // namespace
+
+int la_sms()
 {
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return 148;
     return sms;
 }
 
-}  // namespace
+LaCut la_cut(const LaPlan &plan, int n, bool packed, void *workspace)
+{
+    LaCut c{plan.seg, plan.slots, std::max(1, plan.slots / n), nullptr, nullptr, (float *)workspace};
+    if (packed) {
+        c.next = reinterpret_cast<int *>((char *)workspace + plan.order);
+        c.order = reinterpret_cast<int2 *>(c.next + 4);
+    }
+    return c;
+}
+cudaError_t la_order(const LaSeqs &seqs, const LaCut &cut, int grid, cudaStream_t stream)
+{
+    la_order_kernel<<<1, ORDER_TH, 0, stream>>>(seqs, cut.seg, cut.slots, grid, cut.next, cut.order);
+    return cudaGetLastError();
+}
+cudaError_t la_carry(const LaJobs &jobs, int count, const LaSeqs &seqs, const LaCut &cut, int size, cudaStream_t stream)
+{
+    const int many = seqs.cu != nullptr ? cut.slots - seqs.n : seqs.n;             // sequences that may be cut
+    la_carry_kernel<<<dim3((unsigned)(many * seqs.H), (unsigned)((size + 255) / 256), (unsigned)count), 256, 0, stream>>>(jobs, seqs, cut);
+    return cudaGetLastError();
+}
+void la_plan_slots(LaPlan &plan, const la_shape *s, int jobs, long long units)
+{
+    const long long n = s->cu_seqlens != nullptr ? s->N : s->B;
+    plan.seg = (int)std::min(units * C, 1ll << 30);
+    const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
+    plan.fits = slots * s->H * jobs < (1ll << 30) && s->T < (1ll << 30);
+    plan.slots = plan.fits ? (int)slots : 0;
+    plan.order = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
+    plan.bytes = plan.order + (plan.fits && s->cu_seqlens != nullptr ? 8 * ((size_t)slots + 2) : 0);
+}
 
 // Sequences are cut where there are fewer of them (times heads and jobs) than SMs: the pass for the segments' own states reads K and V once
 // more.  Time in chunks: rounds of units over the SMs, times the chunks of a unit, 1.6 times with the second pass and 6 more for its launches.
 LaPlan la_tc_plan(const la_shape *s, int jobs)
 {
-    const long long n = s->cu_seqlens != nullptr ? s->N : s->B, heads = std::max(1ll, n * s->H * jobs), sms = sm_count();
+    const long long n = s->cu_seqlens != nullptr ? s->N : s->B, heads = std::max(1ll, n * s->H * jobs), sms = la_sms();
     const long long steps = s->cu_seqlens != nullptr ? (n > 0 ? (s->T + n - 1) / n : 0) : s->T, chunks = (steps + C - 1) / C;
     long long best = std::max(1ll, (s->T + C - 1) / C), cost = (heads + sms - 1) / sms * chunks;
     for (long long parts = 2; parts <= 64 && 4 * parts <= chunks; ++parts) {
@@ -1154,13 +1177,8 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
     }
     // Packed sequences: their lengths are the device's.  None of more than twice what an SM has to do, so that no long one holds up the end
     if (s->cu_seqlens != nullptr && n > 1) best = std::min(best, std::max(8ll, 2 * ((s->T / C + n) * s->H * jobs / sms + 1)));
-    LaPlan plan;
-    plan.seg = (int)std::min(best * C, 1ll << 30);
-    const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
-    plan.fits = slots * s->H * jobs < (1ll << 30) && s->T < (1ll << 30);
-    plan.slots = plan.fits ? (int)slots : 0;
-    plan.order = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
-    plan.bytes = plan.order + (plan.fits && s->cu_seqlens != nullptr ? 8 * ((size_t)slots + 2) : 0);
+    LaPlan plan{};
+    la_plan_slots(plan, s, jobs, best);
     return plan;
 }
 
@@ -1209,26 +1227,16 @@ cudaError_t la_tc_run(const la_shape *s, const LaJobs &jobs, int count, const la
     }
     p.seqs = LaSeqs{n, s->H, s->T, s->cu_seqlens, s->log_decay};
     p.jobs = count;
-    p.slots = plan.slots;
-    p.per = std::max(1, plan.slots / n);
-    p.seg = plan.seg;
-    p.carry = (float *)workspace;
+    p.cut = la_cut(plan, n, s->cu_seqlens != nullptr, workspace);
     p.units = plan.slots * s->H * count;
-    const int sms = sm_count();
+    const int sms = la_sms();
     if (s->cu_seqlens != nullptr) {
-        p.next = reinterpret_cast<int *>((char *)workspace + plan.order);
-        p.order = reinterpret_cast<int2 *>(p.next + 4);
-        la_order_kernel<<<1, ORDER_TH, 0, stream>>>(p.seqs, p.seg, p.slots, std::min(p.units, sms), p.next, p.order);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = la_order(p.seqs, p.cut, std::min(p.units, sms), stream);
         if (e != cudaSuccess) return e;
     }
     if (plan.slots > n) {
         cudaError_t e = launch(p, dk, dv, true, sms, stream);
-        if (e != cudaSuccess) return e;
-        const int cut = s->cu_seqlens != nullptr ? plan.slots - n : n;             // sequences that may be
-        la_carry_kernel<<<dim3((unsigned)(cut * s->H), (unsigned)((s->Dk * s->Dv + 255) / 256), (unsigned)count), 256, 0, stream>>>(jobs, p.seqs, p.slots, p.per,
-                                                                                                                            p.seg, p.next, p.order, p.carry);
-        e = cudaGetLastError();
+        if (e == cudaSuccess) e = la_carry(jobs, count, p.seqs, p.cut, s->Dk * s->Dv, stream);
         if (e != cudaSuccess) return e;
     }
     return launch(p, dk, dv, false, sms, stream);

@@ -126,6 +126,17 @@ def test_many_sequences(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 2100, 2, 64, 64), (2, 1500, 1, 128, 96), (1, 1300, 3, 20, 30), (1, 2048, 1, 32, 128), (1, 1999, 1, 40, 7)], ids=str)
+def test_few_long_sequences(size, dtype):
+    """Cut into segments, on either path (widths that are no multiples of 16 take the one of fp32)."""
+    for state in (False, True):
+        x = make(*size, dtype, seed=3, state=state, decays=[-0.003, -0.7, -0.05][:size[2]])
+        o, S = forward(x, 0.2)
+        check_forward(x, o, S, 0.2)
+        check_backward(x, backward(x, 0.2), 0.2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("decays", [[0.0, -30.0], [-1e-6, -100.0], [float("-inf"), -2e-4]], ids=str)
 def test_decays_from_none_to_everything(decays, dtype):
     x = make(1, 270, 2, 64, 64, dtype, decays=decays)
