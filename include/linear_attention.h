@@ -19,7 +19,8 @@
  * written may not overlap one that is read; nor may any other result overlap an input or another result.
  *
  * Types: LA_F32 or LA_BF16 for q, k, v, o and their gradients; sums and states are fp32.  Where bf16 rows lie on 16 bytes (base and strides)
- * and Dk, Dv are multiples of 16, and in la_forward and la_backward only, the products take bf16 factors: the intermediate
+ * and Dk, Dv are multiples of 16, and the sequences are not short (up to 8, 24, 32 or 96 steps on average, by widths and number), and in la_forward and
+ * la_backward only, the products take bf16 factors: the intermediate
  * scores and the state that a chunk starts from are rounded to bf16 before their product, the sums that a state is made of are not (its factors go in
  * two or three bf16 pieces: off by 3e-6 in the first case, which is taken where no state is asked for or the chunk is too far back to be seen in
  * it).  Everywhere else the products are of fp32 values in two pieces of 22 bits together (fewer below 2^-104: what

@@ -1175,8 +1175,8 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
         const long long per = (chunks + parts - 1) / parts, c = (heads * parts + sms - 1) / sms * (per + 1) * 8 / 5 + 6;
         if (c < cost) { cost = c; best = per; }
     }
-    // Packed sequences: their lengths are the device's.  None of more than twice what an SM has to do, so that no long one holds up the end
-    if (s->cu_seqlens != nullptr && n > 1) best = std::min(best, std::max(8ll, 2 * ((s->T / C + n) * s->H * jobs / sms + 1)));
+    // Packed sequences: their lengths are the device's.  None of more than a quarter above what an SM has to do, so that no long one holds up the end
+    if (s->cu_seqlens != nullptr && n > 1) best = std::min(best, std::max(4ll, ((s->T / C + n) * s->H * jobs / sms + 1) * 5 / 4));
     LaPlan plan{};
     la_plan_slots(plan, s, jobs, best);
     return plan;
@@ -1185,6 +1185,13 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
 bool la_tc_takes(const la_shape *s, int jobs, const la_tensor *const *tensors, int count)
 {
     if (s->type != LA_BF16 || s->Dk % 16 || s->Dv % 16 || s->T < 1) return false;
+    // Short sequences leave a chunk of 128 steps mostly empty: up to these lengths (packed: on average) the other path's 32 are faster.  16 heads, bf16,
+    // with states, forward and gradients, us here and there: 200 sequences, widths of 32: 64 steps 111, 346 and 60, 171; 128 steps 112, 347 and
+    // 138, 368; of 64: 20 steps 137, 357 and 121, 300; 48 steps 136, 360 and 191, 502; of 128: 8 steps 285, 671 and 263, 698; 20 steps 286, 673 and
+    // 378, 1026; 4 sequences, widths of 32: 32 steps 10, 14.5 and 9.8, 10; 48 steps 9.3, 14.6 and 13.3, 13.4.
+    const long long n = s->cu_seqlens != nullptr ? s->N : s->B, steps = s->cu_seqlens != nullptr ? s->T / std::max(1ll, n) : s->T;
+    const int widest = std::max(s->Dk, s->Dv);
+    if (steps <= (widest <= 32 ? (n * s->H * jobs > 4 * la_sms() ? 96 : 32) : widest <= 64 ? 24 : 8)) return false;
     for (int i = 0; i < count; ++i) {
         const la_tensor &t = *tensors[i];
         if (reinterpret_cast<uintptr_t>(t.data) & 15u) return false;
