@@ -1160,7 +1160,8 @@ void la_plan_slots(LaPlan &plan, const la_shape *s, int jobs, long long units)
     const long long slots = s->cu_seqlens != nullptr ? s->T / plan.seg + n : n * std::max(1ll, (s->T + plan.seg - 1) / plan.seg);
     plan.fits = slots * s->H * jobs < (1ll << 30) && s->T < (1ll << 30);
     plan.slots = plan.fits ? (int)slots : 0;
-    plan.order = plan.fits && slots > n ? (size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) : 0;
+    // (the order's pairs are read as one: behind states of odd widths too they lie on 16 bytes)
+    plan.order = plan.fits && slots > n ? ((size_t)jobs * slots * s->H * s->Dk * s->Dv * sizeof(float) + 15) / 16 * 16 : 0;
     plan.bytes = plan.order + (plan.fits && s->cu_seqlens != nullptr ? 8 * ((size_t)slots + 2) : 0);
 }
 
