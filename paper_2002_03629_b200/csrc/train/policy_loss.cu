@@ -159,19 +159,11 @@ __device__ __forceinline__ void piece_sum(const Piece<T> &p, float ref, float (&
 #pragma unroll
     for (int e = 0; e < W; ++e) sum[e & 1] += exp_of<T>(x[e], ref);
 }
-// What the gradient's exponentials count against.  fp32: the reference, and a factor -g / sum.  bf16: the factor's logarithm in the reference, its sign
-// put on afterwards, two values at a time.
+// What the gradient's exponentials count against, and what they are multiplied by, -g / sum.  (The factor's logarithm taken into the reference would
+// save the product, but is rounded there to the reference's last bit: a gradient 1 % off where the logits lie near 2e5.)
 struct Against {
     float ref, factor;
-    uint32_t sign;
 };
-template <typename T>
-__device__ __forceinline__ Against gradient_against(float ref, float g, float sum)
-{
-    const float factor = -g / sum;
-    if constexpr (sizeof(T) == 4) return Against{ref, factor, 0u};
-    else return Against{ref - log2f(fabsf(factor)), 1.0f, factor < 0.0f ? 0x80008000u : 0u};
-}
 template <typename T>
 __device__ __forceinline__ Piece<T> piece_gradient(const Piece<T> &p, const Against &a)
 {
@@ -180,11 +172,8 @@ __device__ __forceinline__ Piece<T> piece_gradient(const Piece<T> &p, const Agai
     float x[W];
     p.get(x);
 #pragma unroll
-    for (int e = 0; e < W; ++e) x[e] = sizeof(T) == 4 ? exp_of<T>(x[e], a.ref) * a.factor : exp_of<T>(x[e], a.ref);
+    for (int e = 0; e < W; ++e) x[e] = exp_of<T>(x[e], a.ref) * a.factor;
     out.set(x);
-    if constexpr (sizeof(T) == 2) {
-        out.raw.x ^= a.sign; out.raw.y ^= a.sign; out.raw.z ^= a.sign; out.raw.w ^= a.sign;
-    }
     return out;
 }
 // the action's own value: g on top, rounded once
@@ -307,7 +296,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) rows_kernel(const __grid_co
     if (c.dz == nullptr) return;
     T *const dz = (T *)c.dz + i * c.dstride;
     const bool alike = lead(dz) == -from;
-    const Against g = gradient_against<T>(ref, r.g, total);
+    const Against g{ref, -r.g / total};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int first = from + (k * G + t) * W;
@@ -431,7 +420,7 @@ __global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Ca
             }
             sh.row = r;
             sh.total = all.s;
-            sh.against = gradient_against<T>(sh.ref, r.g, all.s);
+            sh.against = Against{sh.ref, -r.g / all.s};
         }
         __syncthreads();
         const Row r = sh.row;
