@@ -189,10 +189,10 @@ template <typename T>
 __device__ __forceinline__ Sum join(Sum a, Sum b)
 {
     const float m = fmaxf(a.m, b.m), r = reference<T>(against(m));
-    // (a side that has seen nothing has sum 0; a NaN in a sum stays.  Sums count against the reference of their own maximum: the factor is the
-    // quotient of the two references, not of the maxima)
+    // (a side that has seen nothing has sum 0, or NaN, against 0: it stays as it is, for the factor may be infinite.  Sums count against the reference
+    // of their own maximum: the factor is the quotient of the two references, not of the maxima)
     auto moved = [&](Sum x) {
-        if (x.m == m) return x.s;
+        if (x.m == m || x.m == -INFINITY) return x.s;
         if constexpr (sizeof(T) == 4) return x.s * expf(against(x.m) - r);
         else return x.s * exp2f(reference<T>(against(x.m)) - r);
     };
