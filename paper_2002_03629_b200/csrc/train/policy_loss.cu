@@ -105,14 +105,19 @@ __device__ __forceinline__ int lead(const T *row)      // values between the 16-
     return (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
 }
 
-// Exponentials against a reference.  fp32 logits: e^(z - m) to full precision.  bf16 logits: 2^(z log2 e - M) by the special function, off by 2^-22,
-// with M = m log2 e as rounded: the same M stands in the action's own logarithm, so that its rounding cancels.
+// Exponentials against a reference, the largest logit m.  fp32 logits: e^(z - m) to full precision.  bf16 logits: 2^(z log2 e - M) by the special
+// function, off by 2^-22, with M = m log2 e as rounded: the same M stands in the sum, the gradient and the action's own logarithm, so that its rounding cancels.
+// From |m| = 2^15 on, bf16 values next to m lie 128 apart or more: a logit is m itself or has the share e^-128, zero in fp32.  There 2^(z - m) gives
+// the same ones and zeros, and neither product nor rounding leaves fp32, as M and its last bit would (from m = 4e9 on).
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+struct Ref {
+    float by, at;                          // z counts as by * z - at
+};
 template <typename T>
-__device__ __forceinline__ float reference(float m)
+__device__ __forceinline__ Ref reference(float m)
 {
-    if constexpr (sizeof(T) == 4) return m;
-    else return m * LOG2E;
+    if (sizeof(T) == 4 || fabsf(m) >= 0x1p15f) return Ref{1.0f, m};
+    return Ref{LOG2E, m * LOG2E};
 }
 __device__ __forceinline__ float power2(float x)
 {
@@ -121,17 +126,17 @@ __device__ __forceinline__ float power2(float x)
     return y;
 }
 template <typename T>
-__device__ __forceinline__ float exp_of(float z, float ref)
+__device__ __forceinline__ float exp_of(float z, const Ref &ref)
 {
-    if constexpr (sizeof(T) == 4) return expf(z - ref);
-    else return power2(fmaf(z, LOG2E, -ref));
+    if constexpr (sizeof(T) == 4) return expf(z - ref.at);
+    else return power2(fmaf(z, ref.by, -ref.at));
 }
 // z - log sum exp, for the sum s against the reference
 template <typename T>
-__device__ __forceinline__ float log_share(float z, float ref, float s)
+__device__ __forceinline__ float log_share(float z, const Ref &ref, float s)
 {
-    if constexpr (sizeof(T) == 4) return z - ref - logf(s);
-    else return (fmaf(z, LOG2E, -ref) - log2f(s)) * LN2;
+    if (sizeof(T) == 4 || ref.by == 1.0f) return z - ref.at - logf(s);
+    return (fmaf(z, ref.by, -ref.at) - log2f(s)) * LN2;
 }
 
 // What is done with a piece: its maximum (NaN aside), the sum of its exponentials, and those as a piece of the gradient.  (Packed operations on two
@@ -151,7 +156,7 @@ __device__ __forceinline__ float piece_max(const Piece<T> &p)
 }
 // (two sums, so that an addition need not wait for the one before)
 template <typename T>
-__device__ __forceinline__ void piece_sum(const Piece<T> &p, float ref, float (&sum)[2])
+__device__ __forceinline__ void piece_sum(const Piece<T> &p, const Ref &ref, float (&sum)[2])
 {
     constexpr int W = Piece<T>::W;
     float x[W];
@@ -162,7 +167,8 @@ __device__ __forceinline__ void piece_sum(const Piece<T> &p, float ref, float (&
 // What the gradient's exponentials count against, and what they are multiplied by, -g / sum.  (The factor's logarithm taken into the reference would
 // save the product, but is rounded there to the reference's last bit: a gradient 1 % off where the logits lie near 2e5.)
 struct Against {
-    float ref, factor;
+    Ref ref;
+    float factor;
 };
 template <typename T>
 __device__ __forceinline__ Piece<T> piece_gradient(const Piece<T> &p, const Against &a)
@@ -178,7 +184,7 @@ __device__ __forceinline__ Piece<T> piece_gradient(const Piece<T> &p, const Agai
 }
 // the action's own value: g on top, rounded once
 template <typename T>
-__device__ __forceinline__ void put_action(const Call &c, T *dz, int action, float za, float ref, float sum, float g) { put(dz + action, fmaf(exp_of<T>(za, ref), -g / sum, g)); }
+__device__ __forceinline__ void put_action(const Call &c, T *dz, int action, float za, const Ref &ref, float sum, float g) { put(dz + action, fmaf(exp_of<T>(za, ref), -g / sum, g)); }
 
 // A running maximum and the sum of exponentials against it.  While nothing but -infinity has been seen the sum counts against 0.
 struct Sum {
@@ -188,13 +194,15 @@ __device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.0f
 template <typename T>
 __device__ __forceinline__ Sum join(Sum a, Sum b)
 {
-    const float m = fmaxf(a.m, b.m), r = reference<T>(against(m));
+    const float m = fmaxf(a.m, b.m);
+    const Ref r = reference<T>(against(m));
     // (a side that has seen nothing has sum 0, or NaN, against 0: it stays as it is, for the factor may be infinite.  Sums count against the reference
-    // of their own maximum: the factor is the quotient of the two references, not of the maxima)
+    // of their own maximum: the factor is the quotient of the two references, not of the maxima; references of two kinds are 128 apart, e^-128 is none)
     auto moved = [&](Sum x) {
         if (x.m == m || x.m == -INFINITY) return x.s;
-        if constexpr (sizeof(T) == 4) return x.s * expf(against(x.m) - r);
-        else return x.s * exp2f(reference<T>(against(x.m)) - r);
+        const Ref own = reference<T>(against(x.m));
+        if constexpr (sizeof(T) == 4) return x.s * expf(own.at - r.at);
+        else return x.s * (own.by == r.by ? exp2f(own.at - r.at) : 0.0f);
     };
     return Sum{m, moved(a) + moved(b)};
 }
@@ -220,7 +228,7 @@ __device__ __forceinline__ Given given(const Call &c, long long i, const T *z, l
     return g;
 }
 template <typename T>
-__device__ __forceinline__ Row row_numbers(const Call &c, const Given &x, float ref, float sum)
+__device__ __forceinline__ Row row_numbers(const Call &c, const Given &x, const Ref &ref, float sum)
 {
     Row r;
     r.logp = x.known ? log_share<T>(x.za, ref, sum) : NAN;
@@ -271,7 +279,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G) rows_kernel(const __grid_co
         for (int w = 0; w < G / 32; ++w) m = fmaxf(m, sums[w].m);
     }
     // (a row of nothing but -infinity has the sum 0: its logarithm, -infinity - (-infinity), is NaN)
-    const float ref = reference<T>(against(m));
+    const Ref ref = reference<T>(against(m));
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -317,7 +325,8 @@ struct RingShared {
     Sum cta[2][8];
     Row row;
     Against against;
-    float ref, total;
+    Ref ref;
+    float total;
     int dead;
 };
 
@@ -382,7 +391,7 @@ __global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Ca
         m = sh.top[lane % (RTH / 32)];
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        float ref = reference<T>(against(m));
+        Ref ref = reference<T>(against(m));
         float sums[2] = {0.0f, 0.0f};
         if (edge >= 0) piece_sum<T>(part, ref, sums);
 #pragma unroll 2
