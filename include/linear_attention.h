@@ -30,7 +30,8 @@
  *
  * Asynchronous on `stream`, allocates nothing; the same call gives the same bits.  `workspace`: device memory of la_workspace() bytes on
  * 16 bytes, used by this call until its work on the stream is done (calls on different streams, and graphs that may run
- * at the same time, need one each).  Limits: 1 <= Dk, Dv <= LA_MAX_D, H >= 1, B, N >= 0, sequences * H <= 2^24, B * T <= 2^40, T <= 2^31 - 1.
+ * at the same time, need one each).  Limits: 1 <= Dk, Dv <= LA_MAX_D, H >= 1, B, N >= 0, sequences * H <= 2^24, B * T <= 2^40,
+ * T <= LA_MAX_T (the kernels count steps in 32 bits, up to a chunk beyond the last).
  * Waits inside the kernels, for their own copies and products, end after two seconds; outputs that were not written by then are undefined,
  * the states NaN.  Returns LA_OK, LA_ERR_INVALID (nothing is launched) or LA_ERR_CUDA (la_last_error() names the error).
  */
@@ -47,6 +48,7 @@ extern "C" {
 #define LA_ERR_INVALID (-1)
 #define LA_ERR_CUDA (-2)
 #define LA_MAX_D 128
+#define LA_MAX_T ((1ll << 31) - 128)
 #define LA_F32 0
 #define LA_BF16 1
 

@@ -363,7 +363,7 @@ bool shape_ok(const la_shape *s)
 {
     if (s == nullptr || (s->type != LA_F32 && s->type != LA_BF16) || s->log_decay == nullptr) return false;
     if (s->H < 1 || s->Dk < 1 || s->Dk > LA_MAX_D || s->Dv < 1 || s->Dv > LA_MAX_D) return false;
-    if (s->B < 0 || s->T < 0 || s->T > 0x7fffffffll || (s->cu_seqlens != nullptr && (s->B != 1 || s->N < 0))) return false;
+    if (s->B < 0 || s->T < 0 || s->T > LA_MAX_T || (s->cu_seqlens != nullptr && (s->B != 1 || s->N < 0))) return false;
     const long long n = s->cu_seqlens != nullptr ? s->N : s->B;
     return n * s->H <= (1ll << 24) && s->B * s->T <= (1ll << 40) && std::isfinite(s->scale);
 }

@@ -11,6 +11,7 @@ from .binding import JsError, JS_ERR_ARG, load_library, _elsewhere, _stream_ptr,
 
 LA_OK, LA_ERR_INVALID, LA_ERR_CUDA = 0, -1, -2
 LA_MAX_D = 128
+LA_MAX_T = (1 << 31) - 128
 LA_F32, LA_BF16 = 0, 1
 _TYPES = {torch.float32: LA_F32, torch.bfloat16: LA_BF16}
 
@@ -114,7 +115,7 @@ def _shape(q, v, log_decay, scale, cu_seqlens, dims=4):
 def _workspace(s, backward, like):
     n = _lib().la_workspace(s, backward)
     if n == 0:
-        _bad(f"sizes outside the documented limits (1 <= Dk, Dv <= {LA_MAX_D})")
+        _bad(f"sizes outside the documented limits (1 <= Dk, Dv <= {LA_MAX_D}, at most {LA_MAX_T} steps) or a scale that is not finite")
     return like.new_empty((n + 3) // 4), n
 
 

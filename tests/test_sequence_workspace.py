@@ -24,3 +24,20 @@ def test_the_order_of_packed_segments_lies_on_8_bytes(la, T, N, H, Dk, Dv, dtype
     size = lib.la_workspace(C.byref(packed), backward)
     assert size > 4 * H * Dk * Dv                            # (it is cut: the states of more than one segment)
     assert size % 8 == 0
+
+
+def test_the_longest_sequences(la):
+    """Steps are counted in 32 bits, by chunks of 32 and of 128, up to a chunk beyond the last step: 2^31 - 128 of them at most."""
+    lib, most = la._lib(), 2 ** 31 - 128
+    t = la._Tensor(1 << 20, 0, 1, 0)
+    r = C.byref(t)
+    for packed in (False, True):
+        def shape(T):
+            return la._Shape(type=1, B=1, N=1 if packed else 0, T=T, H=1, Dk=1, Dv=1, cu_seqlens=1 << 20 if packed else None, log_decay=1 << 20, scale=1.0)
+        assert lib.la_workspace(C.byref(shape(most)), 0) > 0 and lib.la_workspace(C.byref(shape(most)), 1) > 0
+        for T in (most + 1, 2 ** 31 - 32, 2 ** 31 - 1):
+            s = shape(T)
+            p = C.byref(s)
+            assert lib.la_workspace(p, 0) == 0 and lib.la_workspace(p, 1) == 0
+            assert lib.la_forward(p, r, r, r, None, r, None, 1 << 20, 1 << 30, None) == la.LA_ERR_INVALID
+            assert lib.la_backward(p, r, r, r, None, r, None, r, r, r, None, 1 << 20, 1 << 30, None) == la.LA_ERR_INVALID
