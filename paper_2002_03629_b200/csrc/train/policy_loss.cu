@@ -367,11 +367,13 @@ __global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Ca
         const long long action = c.actions[i];
         Given x{};                                          // (asked for now, needed later; and before anything of the row is written: dlogits may be
         if (tid == 0) x = given(c, i, z, action);          // the logits)
-        // (a wait for this CTA's own copies: it ends, at the latest after MBAR_WAIT_NS, and then the row is NaN)
-        bool here = mbar_try_wait(&sh.full[buf], par);
-        if (!here) {
+        // (a wait for this CTA's own copies: it ends, at the latest after MBAR_WAIT_NS, and then this row and those after it are NaN, whichever thread
+        // gave up, and nothing more is asked for)
+        if (!mbar_try_wait(&sh.full[buf], par) && sh.dead == 0) {
             const uint64_t t0 = global_ns();
+            bool here;
             while (!(here = mbar_try_wait(&sh.full[buf], par)) && global_ns() - t0 < MBAR_WAIT_NS) {}
+            if (!here) sh.dead = 1;
         }
         // pieces that lie in the row from end to end, in shared memory; the row's first and last one may be a part, which one thread each reads
         const int q0 = max(p0, from < 0 ? 1 : 0), q1 = max(q0, min(p1, (c.V - from) / W));
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Ca
             sum = lane < RTH / 32 ? sh.sum[lane] : 0.0f;
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (!here) sum = NAN;
+            if (sh.dead != 0) sum = NAN;
         }
         if (ctas > 1) {
             // every CTA of the cluster gets every other one's sum, and adds them in the same order
@@ -456,9 +458,13 @@ __global__ void __launch_bounds__(RTH, 2) ring_kernel(const __grid_constant__ Ca
             const int k = ((int)action - from) / W;
             if (k >= p0 && k < p1) put_action<T>(c, (T *)c.dz + i * c.dstride, (int)action, x.za, sh.ref, sh.total, r.g);
         }
-        if (tid == 0 && i + bufs * rows < c.N) load(i + bufs * rows, buf);
+        if (tid == 0 && sh.dead == 0 && i + bufs * rows < c.N) load(i + bufs * rows, buf);
         if (++buf == bufs) { buf = 0; par ^= 1u; }
     }
+    // After a wait that gave up: copies on their way, microseconds' worth, end before the shared memory is given back
+    if (sh.dead != 0)
+#pragma unroll 1
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     if (ctas > 1) cluster_sync();
 }
 
