@@ -111,7 +111,10 @@ def _stream_ptr(stream) -> Optional[int]:
 
 
 def _elsewhere(index: int, stream) -> bool:
-    """Does a call on tensors of this device run on another device or stream than the current one?"""
+    """Does a call on tensors of this device run on another device or stream than the current one?  A stream of another device than the tensors' is refused:
+    the kernels would run there, on this device's memory."""
+    if stream is not None and stream.device_index != index:
+        raise JsError(JS_ERR_ARG, f"stream: it belongs to device {stream.device_index}, the tensors to device {index}")
     return stream is not None or index != torch._C._cuda_getDevice()
 
 
