@@ -12,8 +12,7 @@
 //   K, S  eight warps: K from shared memory, transposed on the way, weighted and cut into two or three bf16 pieces (the left operand of
 //         U; one piece would leave the fp32 state off by 2e-3, three leave 5e-7; two, off by 3e-6, do where nobody asks for the state): two into
 //         tensor memory, the third back to where K was.  The state, fp32, in registers, a row of Dv / 2 values a thread; rounded to bf16 into shared
-//         memory for Q S.  Under strong decay they scale Q S by lambda^(i+1) in tensor memory before P V is added.  (They have the time: with the
-//         outputs as their work too, gradients of 8 x 2048 steps took 204 to 220 us, a prompt of 65536 steps 323 to 336.)
+//         memory for Q S, which they scale by lambda^(i+1) in tensor memory before P V is added.
 //   a warp that finds units and loads tiles (TMA, a ring of stages that runs on across chunks and units), one that issues the MMAs
 // Bound: the chain of the roles from one chunk to the next, 4 us a chunk and SM at widths of 128 (tensor pipe active for 30 % of the time, issue slots
 // for 35 %, DRAM for 32 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
@@ -94,7 +93,7 @@ __device__ __forceinline__ bool three_pieces(float log_decay, int n, int c)
 
 // What the roles need to know of a unit.  The loading warp works it out and hands it on through a ring, so that the code that finds
 // units (divisions, searches) is not in every role.
-enum : int { BACK = 1, THREE = 2, WEAK = 4, INIT = 8, TURNED = 16, END = 32 };
+enum : int { BACK = 1, THREE = 2, INIT = 4, TURNED = 8, END = 16 };
 struct alignas(16) Work {
     int flags;                               // THREE: the last state is asked for; INIT: there is a state before the first chunk; TURNED: it lies transposed
     int n, c0, c1;                           // steps of the sequence, chunks [c0, c1) of it
@@ -121,7 +120,7 @@ struct Shared {
     Out out[4];
     uint32_t tmem;
     int dead;
-    // weights of the scores' columns; of K's rows, in fp32 and as two bf16 pieces, rows 2 i and 2 i + 1 in word i.  (A table is written by each
+    // powers of distances for the scores; weights of K's rows, in fp32 and as two bf16 pieces, rows 2 i and 2 i + 1 in word i.  (A table is written by each
     // warp of its group, the same values; no warp is then still at the chunk before, whose products a barrier has reported.)
     alignas(16) float wp[C], wk[C];
     uint32_t wk1[C / 2], wk2[C / 2];
@@ -142,11 +141,9 @@ __device__ __forceinline__ bool la_wait(int &dead, uint64_t *bar, uint32_t parit
 template <typename Sh>
 __device__ __forceinline__ bool warp_wait(Sh &sh, uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, la_wait(sh.dead, bar, parity)); }
 
-// Weak decay: O = lambda^(i+1) (Q S + P' V) with P' = scores * lambda^(-j-1), one weight a column, all powers taken MID steps lower (S times lambda^MID);
-// the sum stays in tensor memory until it is complete.  With lambda^-64 beyond e^44 the products could leave fp32: then P has lambda^(i-j), and
-// Q S is scaled in tensor memory before P V is added.
-constexpr int MID = 64;
-__device__ __forceinline__ float power_of(float log_decay, int n) { return expf((float)n * log_decay); }
+// Weights are powers of distances, 1 at most: P has scores * lambda^(i-j), and Q S is scaled by lambda^(i+1) in tensor memory before P V is added.  (The same in
+// one weight a column, P = scores * lambda^(64-1-j) and outputs times lambda^(i+1-64), saves the scaling and its wait, 3 to 8 % of most calls, but reaches
+// e^44 on either side: scores beyond 2.6e19 became infinite and those below 1e-20 lost their bits.)
 
 // D[tmem] (+)= A[tmem] * B[smem], 128 x N x 16
 __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate)
@@ -419,8 +416,8 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             w.last = job.back && x.n > 0 ? la_power(w.ld, 1) : 1.0f;
             w.from = x.c0 > 0 ? p.cut.carry + (((size_t)x.job * p.cut.slots + x.slot) * p.seqs.H + x.h) * size : job.s0 != nullptr ? job.s0 + state : nullptr;
             w.to = x.last && job.s1 != nullptr ? job.s1 + state : nullptr;
-            w.flags = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (w.ld >= -44.0f / MID ? WEAK : 0) | (w.from != nullptr ? INIT : 0) |
-                      (x.c0 == 0 && job.turned ? TURNED : 0) | (end ? END : 0);
+            w.flags = (job.back ? BACK : 0) | (job.s1 != nullptr ? THREE : 0) | (w.from != nullptr ? INIT : 0) | (x.c0 == 0 && job.turned ? TURNED : 0) |
+                      (end ? END : 0);
             tell(w);
             if (end) break;
 #pragma unroll 1
@@ -534,12 +531,12 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                         const uint64_t sd = desc_mn(s_smem, DK * 128);
 #pragma unroll 2
                         for (int k = 0; k < nk; ++k) umma_bf16(tmu + COL_O, qd + (uint64_t)(k >> 2) * PANEL + (uint64_t)(k & 3) * 2, sd + k * K16, iv, k > 0);
-                        if (!(flags & WEAK)) umma_commit(&sh.qs_done);
+                        umma_commit(&sh.qs_done);
                     }
                     __syncwarp();
                 }
                 wait(&sh.p_ready, par);
-                if (state && !(flags & WEAK)) {
+                if (state) {
                     wait(&sh.o_scaled, o_par);
                     o_par ^= 1u;
                 }
@@ -557,19 +554,18 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
     } else if (warp < 4) {
         // ------------------------------------------------------------- O of the chunk before, and P
         uint32_t par = 0;
-        bool on = true, more = true, due = false;
+        bool on = true, more = true, due = false, tables = false;                  // tables: there for this unit
         Place place;
         Work w{};
-        int c = 0, out_stage = 0, had = -1;                                        // had: rows (and more) that the table is for
+        int c = 0, out_stage = 0;
         // the sum that is still to go out: its steps, factor, place
         int out_rows = 0, out_job = 0, out_t = 0, out_h = 0, out_b = 0;
-        float out_f = 0.0f, full_f = 0.0f;
+        float out_f = 0.0f;
         for (;;) {
             while (more && c == w.c1) {
                 more = place.next(sh, w);
                 c = w.c0;
-                had = -1;
-                if (more) full_f = p.job[w.job].out_scale * (w.flags & WEAK ? power_of(w.ld, (w.flags & BACK ? C - 1 - row : row) + 1 - MID) : 1.0f);
+                tables = false;
             }
             if (due) {
                 // By way of shared memory, where the chunk's Q was, and tensor stores by the loading warp; the sequence's last rows by plain
@@ -618,22 +614,17 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             }
             const bool have = c < w.c1 && more;
             if (have) {
-                const bool back = w.flags & BACK, weak = w.flags & WEAK;
-                const int rows = w.rows(c), late = w.late(c);
+                const bool back = w.flags & BACK;
+                const int rows = w.rows(c);
                 if (on) on = warp_wait(sh, &sh.sc_full, par);
                 if (on) {
                     tc_fence_after();
-                    if (had != 2 * rows + late) {
-                        had = 2 * rows + late;
-                        if (weak) {
-#pragma unroll 1
-                            for (int j = lane; j < C; j += 32) sh.wp[j] = w.sum_scale * power_of(w.ld, MID - (back ? rows - 1 - j : j) - late);
-                        } else {
-                            sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
-                            const float own = w.sum_scale * la_power(w.ld, lane);  // 64 + d: d steps later (back: earlier); the other way there is nothing
-                            sh.wp[64 + lane] = back && lane > 0 ? 0.0f : own;
-                            sh.wp[64 - lane] = !back && lane > 0 ? 0.0f : own;
-                        }
+                    if (!tables) {
+                        tables = true;
+                        sh.wp[lane] = w.sum_scale * la_power(w.ld, back ? lane : 31 - lane);
+                        const float own = w.sum_scale * la_power(w.ld, lane);      // 64 + d: d steps later (back: earlier); the other way there is nothing
+                        sh.wp[64 + lane] = back && lane > 0 ? 0.0f : own;
+                        sh.wp[64 - lane] = !back && lane > 0 ? 0.0f : own;
                         __syncwarp();
                     }
                     // Columns of block b that count: all, those up to (from) the row in its own block, none; and none behind the sequence's end
@@ -642,41 +633,31 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                         const int there = rows - 32 * b;
                         return (b == quad ? own : (back ? b > quad : b < quad) ? 0xffffffffu : 0u) & (there >= 32 ? 0xffffffffu : there <= 0 ? 0u : 0xffffffffu >> (32 - there));
                     };
-                    if (weak) {
 #pragma unroll 1
-                        for (int b = 0; b < 4; b += 2) {                           // (two blocks' scores on their way together)
-                            uint32_t s[32], t[32], words[16];
-                            tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
-                            tmem_ld32_issue(lanes + COL_SC + 32 * b + 32, t);
-                            tmem_wait_ld();
-                            p_weigh(s, sh.wp + 32 * b);
-                            p_words(s, words, kept(b));
-                            tmem_st16(lanes + COL_SC + 16 * b, words);
-                            p_weigh(t, sh.wp + 32 * b + 32);
-                            p_words(t, words, kept(b + 1));
-                            tmem_st16(lanes + COL_SC + 16 * b + 16, words);
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int b = 0; b < 4; ++b) {
-                            uint32_t s[32], words[16];
-                            tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
-                            tmem_wait_ld();
-                            if (b != quad) {
-                                // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
-                                const float f = (back ? b > quad : b < quad) ? la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31) : 0.0f;
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t s[32], words[16];
+                        if (back ? b < quad : b > quad) {                          // beyond the diagonal
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
-                                p_weigh(s, sh.wp);
-                            } else {
-                                // the row's own block: the power of the distance
-                                const float *const own = sh.wp + 64 + lane;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * own[-e]);
-                            }
-                            p_words(s, words, kept(b));
+                            for (int e = 0; e < 16; ++e) words[e] = 0;
                             tmem_st16(lanes + COL_SC + 16 * b, words);
+                            continue;
                         }
+                        tmem_ld32_issue(lanes + COL_SC + 32 * b, s);
+                        tmem_wait_ld();
+                        if (b != quad) {
+                            // columns 32 b + e: lambda^(distance to the block's near edge) * lambda^(distance from there)
+                            const float f = la_power(w.ld, back ? 32 * b - row : row - 32 * b - 31);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f);
+                            p_weigh(s, sh.wp);
+                        } else {
+                            // the row's own block: the power of the distance
+                            const float *const own = sh.wp + 64 + lane;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * own[-e]);
+                        }
+                        p_words(s, words, kept(b));
+                        tmem_st16(lanes + COL_SC + 16 * b, words);
                     }
                     tmem_wait_st();
                     tmem_arrive(&sh.p_ready);
@@ -688,9 +669,7 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             out_t = w.step(c);
             out_h = w.h;
             out_b = w.b;
-            out_f = full_f;
-            if ((w.flags & WEAK) && (out_rows != C || !w.late(c)))
-                out_f = row < out_rows ? p.job[w.job].out_scale * power_of(w.ld, (w.flags & BACK ? out_rows - 1 - row : row) + w.late(c) - MID) : 0.0f;
+            out_f = p.job[w.job].out_scale;
             due = true;
             par ^= 1u;
             ++c;
@@ -718,7 +697,6 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
             const int Dk = p.job[w.job].Dk, Dv = p.job[w.job].Dv;
             const bool have = mine && row < Dk;
             const LaStep whole(w.ld, C);
-            const float mid = w.flags & WEAK ? power_of(w.ld, MID) : 1.0f;
             int had = 0;                                                           // rows that the tables are for
 #pragma unroll
             for (int v = 0; v < HV / 2; ++v) S[v] = 0;
@@ -780,36 +758,34 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                 if (w.state(c)) {
                     // the state before the chunk to shared memory, in bf16, for Q S (whose last product has met the one before it: sc_full came after)
                     if (mine) {
-                        const f2 mm = pair(mid, mid);
 #pragma unroll
                         for (int v = 0; v < HV; v += 8) {
                             uint32_t r[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) r[e] = narrow(mul2(S[v / 2 + e], mm));
+                            for (int e = 0; e < 4; ++e) r[e] = narrow(S[v / 2 + e]);
                             sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), r[0], r[1], r[2], r[3]);
                         }
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.s_ready);
-                    if (!(w.flags & WEAK)) {                                       // Q S times lambda^(i+1), a row a thread, while the scores become P
-                        on = warp_wait(sh, &sh.qs_done, qs_par);
-                        qs_par ^= 1u;
-                        if (!on) break;
-                        tc_fence_after();
-                        const float g = row < rows ? la_power(w.ld, (w.flags & BACK ? rows - 1 - row : row) + w.late(c)) : 0.0f;
+                    // Q S times lambda^(i+1), a row a thread, while the scores become P
+                    on = warp_wait(sh, &sh.qs_done, qs_par);
+                    qs_par ^= 1u;
+                    if (!on) break;
+                    tc_fence_after();
+                    const float g = row < rows ? la_power(w.ld, (w.flags & BACK ? rows - 1 - row : row) + w.late(c)) : 0.0f;
 #pragma unroll 1
-                        for (int v = v0; v < min(v0 + HV, Dv); v += 32) {          // (columns beyond Dv hold something or other)
-                            uint32_t r[32];
-                            tmem_ld32_issue(lanes + COL_O + v, r);
-                            tmem_wait_ld();
+                    for (int v = v0; v < min(v0 + HV, Dv); v += 32) {              // (columns beyond Dv hold something or other)
+                        uint32_t r[32];
+                        tmem_ld32_issue(lanes + COL_O + v, r);
+                        tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
-                            tmem_st32(lanes + COL_O + v, r);
-                        }
-                        tmem_wait_st();
-                        tmem_arrive(&sh.o_scaled);
+                        for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * g);
+                        tmem_st32(lanes + COL_O + v, r);
                     }
+                    tmem_wait_st();
+                    tmem_arrive(&sh.o_scaled);
                 }
                 on = warp_wait(sh, &sh.u_full, par);
                 par ^= 1u;
