@@ -1,6 +1,6 @@
 /*
  * adamw.h - C ABI of the AdamW step over many tensors at once, with states in 32 or in 8 bits.  It takes what the recurrent network's
- * parameter gradients (rnn_bptt.h) and the other gradients of this library leave behind.
+ * parameter gradients (rnn_bptt.h: one of each sequence, which the caller adds up) and the other gradients of this library leave behind.
  *
  * Step t = 1, 2, ... on every value p with gradient g (fp32 arithmetic, each operation rounded once, nothing fused):
  *     g' = g * grad_scale
@@ -20,7 +20,10 @@
  *            never becomes zero.  r: the low 16 bits for m, the high ones for v, of
  *                x = place + seed * A (32 bits, the place's upper half times B added);  x = (x ^ x >> 16) * A;  x = (x ^ x >> 15) * B;  x = (x ^ x >> 16) * C;  x ^= x >> 15
  *            with A, B, C = 0x6A09E667, 0xBB67AE85, 0x3C6EF373.
- *   A gradient that is not finite makes its value's state NaN, in 8 bits that of its whole block.
+ *            What this does to a step: under steady normal gradients (b2 = 0.99 or 0.999) sqrt(v) is right in the mean within 1 %, and spreads by 15 % about the
+ *            state in 32 bits (5 % of the values below 0.78 of it, 5 % above 1.27): a random factor on each value's step.  m is off by 9 % of its size.
+ *   A gradient g' that is not finite, or whose square is not (from 1.8e19 on): in 32 bits its value's state and parameter become what the formulas give,
+ *   infinite or NaN; in 8 bits the state of its whole block becomes NaN, and the block's parameters with the next step.  `skip` is there to avoid it.
  *
  * Conventions.  `tensors` and the plain numbers are host memory, read before the call returns; everything else is device memory owned
  * by the caller; p, g and copy need no more than their type's alignment (on 16 bytes they are read and written faster).  Tensors must not

@@ -19,12 +19,12 @@
  * written may not overlap one that is read; nor may any other result overlap an input or another result.
  *
  * Types: LA_F32 or LA_BF16 for q, k, v, o and their gradients; sums and states are fp32.  Where bf16 rows lie on 16 bytes (base and strides)
- * and Dk, Dv are multiples of 16, and the sequences are not short (up to 8, 24, 32 or 96 steps on average, by widths and number), and in la_forward and
- * la_backward only, the products take bf16 factors: the intermediate
- * scores and the state that a chunk starts from are rounded to bf16 before their product, the sums that a state is made of are not (its factors go in
- * two or three bf16 pieces, fewer bits below 2^-110: off by 3e-6 in the first case, which is taken where no state is asked for or what comes from the
- * chunk has decayed by e^-6 since; zeros behind it do not bring the third piece back).  Everywhere else the products are of fp32 values in two pieces of 22 bits together (fewer below 2^-104: what
- * lies under 2^-136 is lost; magnitudes from 3.402e38 on count as infinite).
+ * and Dk, Dv are multiples of 16, and the sequences are not short (up to 8, 24, 32 or 96 steps on average, by widths and number; the gradients count as
+ * three times the number, so a forward call and its gradients may take different paths), and in la_forward and la_backward only, the products take
+ * bf16 factors: the intermediate scores and the state that a chunk starts from are rounded to bf16 before their product, the sums that a state is made
+ * of are not (its factors go in two or three bf16 pieces, fewer bits below 2^-110: off by 3e-6 in the first case, which is taken where no state is asked
+ * for or what comes from the chunk has decayed by e^-6 since; zeros behind it do not bring the third piece back).  Everywhere else the products are of
+ * fp32 values in two pieces of 22 bits together (fewer below 2^-104: what lies under 2^-136 is lost; magnitudes from 3.402e38 on count as infinite).
  * Values that are not finite: outputs of the chunk of up to 128 steps that holds one, and everything that depends on it, are not specified; no
  * other sequence and no other head is touched.
  *

@@ -17,7 +17,8 @@
  * Conventions.  Device pointers, row-major, rows of logits and dlogits `stride` values apart; no alignment but the type's (rows whose logits
  * and dlogits lie alike against 16 bytes are read and written faster).  dlogits may be the logits' own memory (same stride); NULL: no gradient.
  * ref_logp NULL: no KL term.  weights NULL: 1 / N each.  Asynchronous on `stream`, allocates nothing, one launch, no atomics:
- * the same call gives the same bits.  N >= 0, 1 <= V <= PL_MAX_V.  Returns PL_OK, PL_ERR_INVALID (nothing is launched) or PL_ERR_CUDA.
+ * the same call gives the same bits.  Waits inside the kernel, for its own copies of long rows, end after two seconds; the rows that they were for are
+ * NaN.  N >= 0, 1 <= V <= PL_MAX_V.  Returns PL_OK, PL_ERR_INVALID (nothing is launched) or PL_ERR_CUDA.
  */
 #ifndef POLICY_LOSS_H
 #define POLICY_LOSS_H

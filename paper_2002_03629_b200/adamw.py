@@ -97,7 +97,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
                lr: Union[float, torch.Tensor], betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                copies: Optional[Sequence[torch.Tensor]] = None, grad_scale: Optional[torch.Tensor] = None,
                skip: Optional[torch.Tensor] = None, seed: Optional[int] = None, stream=None) -> None:
-    """One step on all tensors, in place.
+    """One step on all tensors, in place (parameters that require gradients too: autograd is told nothing of it).
 
     params      float32, contiguous, no two the same; grads of the same sizes, all float32 or all bfloat16, contiguous
     state       from ``adamw_state`` (or a tuple laid out like it)

@@ -1162,10 +1162,12 @@ LaPlan la_tc_plan(const la_shape *s, int jobs)
 bool la_tc_takes(const la_shape *s, int jobs, const la_tensor *const *tensors, int count)
 {
     if (s->type != LA_BF16 || s->Dk % 16 || s->Dv % 16 || s->T < 1) return false;
-    // Short sequences leave a chunk of 128 steps mostly empty: up to these lengths (packed: on average) the other path's 32 are faster.  16 heads, bf16,
-    // with states, forward and gradients, us here and there: 200 sequences, widths of 32: 64 steps 111, 346 and 60, 171; 128 steps 112, 347 and
-    // 138, 368; of 64: 20 steps 137, 357 and 121, 300; 48 steps 136, 360 and 191, 502; of 128: 8 steps 285, 671 and 263, 698; 20 steps 286, 673 and
-    // 378, 1026; 4 sequences, widths of 32: 32 steps 10, 14.5 and 9.8, 10; 48 steps 9.3, 14.6 and 13.3, 13.4.
+    // Short sequences leave a chunk of 128 steps mostly empty: up to these lengths (packed: on average, rows of no sequence included) the other path's
+    // 32 are faster.  bf16, with states, forward and gradients, us here and there: 200 sequences of 16 heads, widths of 32: 64 steps 111, 388 and 61, 171; 96 steps
+    // 113, 415 and 97, 273; 128 steps 112, 399 and 139, 365; of 64: 24 steps 142, 374 and 122, 309; 48 steps 141, 364 and 191, 503; of 128: 8 steps 288, 694 and 263, 700;
+    // 9 steps 288, 693 and 289, 772; 4 sequences of 16 heads, widths of 32: 32 steps 8.9, 14.0 and 9.4, 9.4; 48 steps 8.9, 14.5 and 13.0, 13.5; of 64: 25 steps 9.6,
+    // 15.5 and 8.9, 13.5.  Forward and gradients share a border, and 2 heads and 32 that of 16: next to it either may be the slower one, by up to a fifth
+    // (gradients of 4 sequences, 32 heads: by two fifths).
     const long long n = s->cu_seqlens != nullptr ? s->N : s->B, steps = s->cu_seqlens != nullptr ? s->T / std::max(1ll, n) : s->T;
     const int widest = std::max(s->Dk, s->Dv);
     if (steps <= (widest <= 32 ? (n * s->H * jobs > 4 * la_sms() ? 96 : 32) : widest <= 64 ? 24 : 8)) return false;

@@ -4,10 +4,11 @@
 // function unit makes at 16 a cycle and SM.  A row is read in pieces of 16 bytes that lie on 16 bytes: rows of odd length begin and end
 // inside a piece, whose values are then read one by one.
 //   rows_kernel   a row's pieces stay in the registers of 32 or 256 threads
-//   ring_kernel   longer rows: a persistent CTA keeps a ring of rows in shared memory, filled by bulk copies, so that the next rows are on their
-//                 way while one is summed and its gradient written.  Rows that leave no room for two, and few rows, are shared by the CTAs of a
-//                 cluster, which exchange maximum and sum through distributed shared memory.
-// Measured: 8192 rows of 50001 bf16, the ring: 324 us, 5.1 TB/s (a row is walked three times, for maximum, sum and gradient, in shared memory; issue slots 47 %,
+//   ring_kernel   longer rows: a persistent CTA keeps a ring of rows in 108 KB of shared memory, filled by bulk copies.  Up to 27648 bf16 or 13824 fp32
+//                 values there is room for two rows and more, and the next ones are on their way while one is summed and its gradient written;
+//                 beyond that only the SM's other CTA works while one loads.  Rows that leave no room for one (55296, 27648), and few rows, are
+//                 shared by the CTAs of a cluster, which exchange maximum and sum through distributed shared memory.
+// Measured: 8192 rows of 50001 bf16, the ring: 327 us, 5.0 TB/s (a row is walked three times, for maximum, sum and gradient, in shared memory; issue slots 47 %,
 // DRAM 59 %; one CTA an SM with a ring twice as long: 376); 1024 rows of 256 fp32, registers: 3 us, the launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -1,4 +1,5 @@
-"""Binding of linear attention with a decay for each head (``include/linear_attention.h``): argument marshalling only."""
+"""Binding of linear attention with a decay for each head (``include/linear_attention.h``): argument marshalling only.  Autograd does not see these calls:
+results of inputs that require gradients carry none; ``linear_attention_backward`` computes them."""
 from __future__ import annotations
 
 import ctypes as C

@@ -1,4 +1,5 @@
-"""Binding of the clipped policy loss with its gradient (``include/policy_loss.h``): argument marshalling only."""
+"""Binding of the clipped policy loss with its gradient (``include/policy_loss.h``): argument marshalling only.  Autograd does not see the call:
+loss and logp carry no gradients, ``dlogits`` is the gradient."""
 from __future__ import annotations
 
 import ctypes as C
