@@ -142,7 +142,7 @@ template <typename Sh>
 __device__ __forceinline__ bool warp_wait(Sh &sh, uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, la_wait(sh.dead, bar, parity)); }
 
 // Weights are powers of distances, 1 at most: P has scores * lambda^(i-j), and Q S is scaled by lambda^(i+1) in tensor memory before P V is added.  (The same in
-// one weight a column, P = scores * lambda^(64-1-j) and outputs times lambda^(i+1-64), saves the scaling and its wait, 3 to 8 % of most calls, but reaches
+// one weight a column, P = scores * lambda^(64-1-j) and outputs times lambda^(i+1-64), saves the scaling, up to 5 % of a call, but reaches
 // e^44 on either side: scores beyond 2.6e19 became infinite and those below 1e-20 lost their bits.)
 
 // D[tmem] (+)= A[tmem] * B[smem], 128 x N x 16
@@ -503,6 +503,19 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     umma_commit(&sh.sc_full);
                 }
                 __syncwarp();
+                // Q S next: it is done, and can be scaled, by the time that K's pieces are there
+                if (!first) wait(&sh.o_free, par ^ 1u);
+                if (state) {
+                    wait(&sh.s_ready, s_par);
+                    s_par ^= 1u;
+                    if (on && elect_one()) {
+                        const uint64_t sd = desc_mn(s_smem, DK * 128);
+#pragma unroll 2
+                        for (int k = 0; k < nk; ++k) umma_bf16(tmu + COL_O, qd + (uint64_t)(k >> 2) * PANEL + (uint64_t)(k & 3) * 2, sd + k * K16, iv, k > 0);
+                        umma_commit(&sh.qs_done);
+                    }
+                    __syncwarp();
+                }
                 wait(&sh.k_ready, par);
                 if (!first) wait(&sh.u_free, par ^ 1u);
                 if (on && elect_one()) {
@@ -520,18 +533,6 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
 #pragma unroll 2
                         for (int k = 0; k < C / 16; ++k) umma_bf16(tmu + COL_U, kd + k * K16, vd + k * K16, iv | (1u << 15), true);
                         umma_commit(&sh.u_full);
-                    }
-                    __syncwarp();
-                }
-                if (!first) wait(&sh.o_free, par ^ 1u);
-                if (state) {
-                    wait(&sh.s_ready, s_par);
-                    s_par ^= 1u;
-                    if (on && elect_one()) {
-                        const uint64_t sd = desc_mn(s_smem, DK * 128);
-#pragma unroll 2
-                        for (int k = 0; k < nk; ++k) umma_bf16(tmu + COL_O, qd + (uint64_t)(k >> 2) * PANEL + (uint64_t)(k & 3) * 2, sd + k * K16, iv, k > 0);
-                        umma_commit(&sh.qs_done);
                     }
                     __syncwarp();
                 }
@@ -720,6 +721,21 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
 #pragma unroll 1
             for (int c = w.c0; c < w.c1; ++c) {
                 const int rows = w.rows(c);
+                if (w.state(c) && on) {
+                    // the state before the chunk to shared memory, in bf16, for Q S (whose product with the one before it this warp has seen done)
+                    if (mine) {
+#pragma unroll
+                        for (int v = 0; v < HV; v += 8) {
+                            uint32_t r[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) r[e] = narrow(S[v / 2 + e]);
+                            sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), r[0], r[1], r[2], r[3]);
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.s_ready);
+                }
                 if (on) on = warp_wait(sh, &sh.full[stage], full_par);
                 if (!on) break;
                 if (rows != had) {                                                 // (this warp has seen the chunk before's products complete)
@@ -756,19 +772,6 @@ __global__ void __launch_bounds__(TH, 1) la_tc_kernel(const __grid_constant__ Pa
                     if (lane == 0) mbar_arrive(&sh.low_ready);
                 }
                 if (w.state(c)) {
-                    // the state before the chunk to shared memory, in bf16, for Q S (whose last product has met the one before it: sc_full came after)
-                    if (mine) {
-#pragma unroll
-                        for (int v = 0; v < HV; v += 8) {
-                            uint32_t r[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) r[e] = narrow(S[v / 2 + e]);
-                            sts128(s_row + ((uint32_t)(((v0 & 63) + v) << 1) ^ s_turn), r[0], r[1], r[2], r[3]);
-                        }
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.s_ready);
                     // Q S times lambda^(i+1), a row a thread, while the scores become P
                     on = warp_wait(sh, &sh.qs_done, qs_par);
                     qs_par ^= 1u;
@@ -1163,10 +1166,10 @@ bool la_tc_takes(const la_shape *s, int jobs, const la_tensor *const *tensors, i
 {
     if (s->type != LA_BF16 || s->Dk % 16 || s->Dv % 16 || s->T < 1) return false;
     // Short sequences leave a chunk of 128 steps mostly empty: up to these lengths (packed: on average, rows of no sequence included) the other path's
-    // 32 are faster.  bf16, with states, forward and gradients, us here and there: 200 sequences of 16 heads, widths of 32: 64 steps 111, 388 and 61, 171; 96 steps
-    // 113, 415 and 97, 273; 128 steps 112, 399 and 139, 365; of 64: 24 steps 142, 374 and 122, 309; 48 steps 141, 364 and 191, 503; of 128: 8 steps 288, 694 and 263, 700;
-    // 9 steps 288, 693 and 289, 772; 4 sequences of 16 heads, widths of 32: 32 steps 8.9, 14.0 and 9.4, 9.4; 48 steps 8.9, 14.5 and 13.0, 13.5; of 64: 25 steps 9.6,
-    // 15.5 and 8.9, 13.5.  Forward and gradients share a border, and 2 heads and 32 that of 16: next to it either may be the slower one, by up to a fifth
+    // 32 are faster.  bf16, with states, forward and gradients, us here and there: 200 sequences of 16 heads, widths of 32: 64 steps 108, 351 and 61, 171; 96 steps
+    // 109, 362 and 98, 273; 128 steps 109, 353 and 139, 365; of 64: 24 steps 132, 352 and 121, 308; 48 steps 131, 358 and 191, 502; of 128: 8 steps 279, 666 and 263, 699;
+    // 9 steps 279, 665 and 289, 771; 4 sequences of 16 heads, widths of 32: 32 steps 8.4, 14.2 and 9.2, 9.4; 48 steps 8.4, 14.3 and 12.6, 13.1; of 64: 25 steps 9.4,
+    // 15.0 and 8.9, 13.5.  Forward and gradients share a border, and 2 heads and 32 that of 16: next to it either may be the slower one, by up to a sixth
     // (gradients of 4 sequences, 32 heads: by two fifths).
     const long long n = s->cu_seqlens != nullptr ? s->N : s->B, steps = s->cu_seqlens != nullptr ? s->T / std::max(1ll, n) : s->T;
     const int widest = std::max(s->Dk, s->Dv);
