@@ -14,10 +14,10 @@
 //         tensor memory, the third back to where K was.  The state, fp32, in registers, a row of Dv / 2 values a thread; rounded to bf16 into shared
 //         memory for Q S, which they scale by lambda^(i+1) in tensor memory before P V is added.
 //   a warp that finds units and loads tiles (TMA, a ring of stages that runs on across chunks and units), one that issues the MMAs
-// Bound: the chain of the roles from one chunk to the next, 4 us a chunk and SM at widths of 128 (tensor pipe active for 30 % of the time, issue slots
-// for 35 %, DRAM for 32 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
-// Measured, bf16, 16 heads of 128: one prompt of 65536 steps 335 us (own states 81, their chain 9, outputs 245; 1.07 GB, 3.2 TB/s); gradients of 8 x 2048
-// steps 204 us; 20 packed prompts of 1 to 2500 steps 97 us (196 with the units dealt out beforehand).
+// Bound: the chain of the roles from one chunk to the next, 4 us a chunk and SM at widths of 128 (tensor pipe active for 29 % of the time, issue slots
+// for 28 %, DRAM for 34 %; the chunk's 128 KB alone would take 2.9).  A second chunk in flight has no room: tensor memory is full, and so is shared memory.
+// Measured, bf16, 16 heads of 128: one prompt of 65536 steps 295 to 311 us (own states 81, their chain 9; 1.07 GB, 3.5 TB/s; 345 to 360 once the power cap has
+// taken the clock from 1965 to 1600 MHz); gradients of 8 x 2048 steps 200 to 210 us; 20 packed prompts of 1 to 2500 steps 104 us.
 // Tensor memory is full: scores and P over them, U, O and K's pieces take 128 columns each.
 // The roles' loops are kept short and free of what can be done once: unrolled further, or with the search for units in each of them, their code
 // fell out of the instruction cache.  setmaxnreg for one role with a whole row of the state a thread was slower (20 warps, spills in others).
